@@ -361,7 +361,7 @@ def _own_attend(s):
     from paper_2607_00501_amd import binding as B
     if "workspace" not in s:
         nb = B.qattn_paged_workspace_bytes(s["case"]["hq"], s["case"]["hkv"], s["case"]["d"], s["case"]["n"],
-                                           s["tokens"], s["case"]["prefix"])
+                                           s["tokens"], s["case"]["prefix"] // s["case"]["page"])
         s["workspace"] = torch.empty(max(nb, 16), dtype=torch.uint8, device=DEV)
     s["out"] = B.qattn_paged_f16(s["q"], s["k_pages"], s["v_pages"], s["tables"], s["offsets"], s["kv_lens"],
                                  s["scale"], prefix=s["prefix"], out=s.get("out"), workspace=s["workspace"])
