@@ -483,6 +483,110 @@ qm_status qdec_cast_f16(const float* x, int64_t n, uint16_t* out, void* stream);
 qm_status qdec_argmax(const float* logits, int64_t n, int32_t* token, void* workspace, size_t ws_bytes,
                       void* stream);
 
+/* Greedy sampling of a batch: tokens[r] = qdec_argmax of row r of logits
+ * (fp32 [rows][n], device), r < rows.  tokens: int32 [rows]; 0 <= rows <= 32768;
+ * workspace: rows x QDEC_ARGMAX_WORKSPACE_BYTES (host-only query
+ * qdec_argmax_rows_workspace_bytes), 4-byte aligned, contents not preserved.
+ * One launch for n <= 4096, else two.
+ * (Sec. 3.2: sampling kernel of the decode step, for several sequences.) */
+qm_status qdec_argmax_rows_workspace_bytes(int64_t rows, size_t* bytes);
+qm_status qdec_argmax_rows(const float* logits, int64_t rows, int64_t n, int32_t* tokens, void* workspace,
+                           size_t ws_bytes, void* stream);
+
+/* ---- Batched serving over a paged KV cache (Sec. 3.2: the cache memory is
+ * laid down before the loop; here in pages that requests of any length share).
+ *
+ * A cache is two pools, fp16 [n_pages][n_kv_heads][page_size][head_dim]; one
+ * page table serves every layer's pools.  page_size: 16, 32, 64, 128 or 256
+ * tokens; 1 <= n_pages < 2^31.  Request i < n_req (1 .. 1024) keeps its token
+ * at position p in row p % page_size of page tables[i][p / page_size]
+ * (int32 [n_req][max_pages], 1 <= max_pages <= 2^20).  Slot: page * page_size
+ * + row.  The tokens of a step lie one after the other, request i's at
+ * offsets[i] .. offsets[i+1] - 1.  Lengths, tables and offsets are read on the
+ * device only, so a captured step can be replayed while they move on.
+ *
+ * A prefix that all requests share (one system prompt) takes the first
+ * prefix_pages entries of every page table; it is whole pages. */
+
+/* The bookkeeping of one step, in one launch.  Request i holds lens[i] tokens;
+ * new_lens[i] >= 0 new ones come, or new_lens[i] < 0: the request has ended.
+ * free_ring (int32 [n_pages]) is a ring of free page ids, ring = {head, count}:
+ * entry j < count at (head + j) % n_pages.
+ *  - Pages: a request takes the pages that its new tokens need from the ring,
+ *    in request order, and they are written into tables from entry
+ *    ceil(lens[i] / page_size) on.  It is refused when they are not there (as is
+ *    every later request that needs any), when its tokens would pass
+ *    max_pages x page_size or when they do not all fit in max_tokens.
+ *  - lens_out[i] = lens[i] + new_lens[i] (refused: lens[i]; ended: 0);
+ *    kv_lens[i] = lens[i] + new_lens[i] (refused or ended: 0), the keys that the
+ *    request's last token attends to; refused[0] = number of refused requests.
+ *  - offsets (int32 [n_req + 1]): sums of the new_lens >= 0, at most max_tokens;
+ *    refused requests keep their place.
+ *  - positions (int32 [max_tokens]) and slots (int64 [max_tokens]) of the
+ *    tokens; -1 for refused requests' tokens and behind the last one.
+ *  - An ended request's pages from entry prefix_pages on go back behind the
+ *    ring's last entry, in request order, free from the next step on.
+ *  - ring_out = the ring's head and count after the step.
+ * tables and free_ring are changed in place, and the same call repeated (same
+ * lens, ring) does the same.  lens_out and ring_out must not be lens and ring.
+ * A length below 0 or past the table is refused, its pages are not given back;
+ * a ring that is none of this size counts as empty.
+ * 0 <= max_tokens <= 65536; 0 <= prefix_pages <= max_pages.  int32 pointers
+ * 4-byte, slots 8-byte aligned.  Deterministic. */
+qm_status qkv_plan(const int32_t* lens, const int32_t* new_lens, int64_t n_req, int32_t page_size, int32_t* tables,
+                   int64_t max_pages, int64_t prefix_pages, int32_t* free_ring, const int32_t* ring, int64_t n_pages,
+                   int64_t max_tokens, int32_t* lens_out, int32_t* kv_lens, int32_t* offsets, int32_t* positions,
+                   int64_t* slots, int32_t* ring_out, int32_t* refused, void* stream);
+
+/* RoPE and the cache append of a step's tokens r < tokens (0 .. 65536) at
+ * their positions and slots (qkv_plan's):
+ *   q_out[r][h] = fp16(rope(q[r][h])), and row slots[r] of the pools the rotated
+ *   keys and the values of token r,
+ * rotation, interleaved columns and per-head norms as qdec_rope_append_rows,
+ * with the same bits.  q: fp32 [tokens][n_q_heads * head_dim], k, v: fp32
+ * [tokens][n_kv_heads * head_dim]; q_out: fp16 [tokens][n_q_heads][head_dim].
+ * table: (cos, sin) pairs of table_len positions (qdec_rope_table).  A token
+ * whose slot is not in the pools or whose position is not in the table (-1)
+ * writes nothing; no two tokens may have the same slot.  head_dim 64 or 128.
+ * q, k, v 16-byte, positions 4-byte, the others 8-byte aligned.
+ * (Sec. 3.2: RoPE and the KV cache.) */
+qm_status qkv_rope_append(const float* q, const float* k, const float* v, int32_t n_q_heads, int32_t n_kv_heads,
+                          int32_t head_dim, int64_t tokens, const int32_t* positions, const int64_t* slots,
+                          int32_t interleaved, const uint16_t* q_norm, const uint16_t* k_norm, float eps,
+                          const float* table, int64_t table_len, uint16_t* q_out, uint16_t* k_pages,
+                          uint16_t* v_pages, int64_t n_pages, int32_t page_size, void* stream);
+
+/* Causal attention of a step's tokens over the paged cache (Sec. 3.4:
+ * attention over key tiles with a running maximum and sum; Sec. 3.2: the KV
+ * cache): prompts, chunks of prompts and single tokens in one call.  Token j of
+ * request i, of t_i = offsets[i+1] - offsets[i], attends to the first
+ * n = kv_lens[i] - t_i + j + 1 keys of its request:
+ *   out[offsets[i] + j][h] = fp16_RNE(sum_{p<n} w_p v[g][p]),
+ *   w = softmax_p(scale * q[h] . k[g][p]),  g = h / (n_q_heads / n_kv_heads);
+ * a row that sees no key (kv_lens[i] = 0) is 0.  What lies past a row's keys
+ * does not reach it, infinities and NaNs included.
+ * prefix_pages > 0: positions below prefix_pages * page_size are read from the
+ * pages prefix[0 .. prefix_pages), once for all requests, and the tables'
+ * entries for them are not read; the other keys as before.
+ * q: fp16 [tokens][n_q_heads][head_dim]; out: fp16 [tokens][n_q_heads *
+ * head_dim] (the output projection's rows); rows past offsets[n_req] are left
+ * as they were.  head_dim 64 or 128; n_kv_heads <= 128; n_q_heads <= 1024, a
+ * multiple of it; 0 <= tokens <= 65536; scale finite and > 0.  A page id
+ * outside [0, n_pages) among the keys that a 128-row tile of (token, head)
+ * pairs sees makes that tile's rows NaN (no host synchronisation, so no status
+ * code).  Scores, maxima and sums in fp32; the weights go to the MFMA in fp16
+ * (to nearest).  Two launches.  Deterministic.
+ * q, pools, out and workspace 16-byte aligned; workspace of at least
+ * qattn_paged_workspace_bytes for this n_req, tokens and prefix_pages (device
+ * scratch, contents not preserved; calls that share it must not overlap). */
+qm_status qattn_paged_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_req,
+                                      int64_t tokens, int64_t prefix_pages, size_t* bytes);
+qm_status qattn_paged_f16(const uint16_t* q, const uint16_t* k_pages, const uint16_t* v_pages, int64_t n_pages,
+                          int32_t page_size, const int32_t* tables, int64_t max_pages, const int32_t* prefix,
+                          int64_t prefix_pages, const int32_t* offsets, const int32_t* kv_lens, int64_t n_req,
+                          int64_t tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                          uint16_t* out, void* workspace, size_t ws_bytes, void* stream);
+
 /* Host-only: workspace bytes qmoe_grouped_gemm needs for m tokens, so the
  * caller allocates it once for the largest chunk (Sec. 3.2: no allocation on
  * the hot path; Sec. 3.4: bounded prefill chunks).  Covers h and the

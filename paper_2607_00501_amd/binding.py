@@ -33,7 +33,9 @@ EXPORTS = ("qm_last_error", "qm_weight_bytes", "qm_quantise", "qm_dequantise", "
            "qdec_argmax", "qmatmul_gemv_swiglu_f16", "qattn_decode_f16", "qmatmul_gemv_grouped_rmsnorm",
            "qmatmul_gemv_swiglu_rmsnorm_f16", "qdec_rope_table", "qdec_rope_table_llama3",
            "qmatmul_gemv_qkv_rmsnorm_rope", "qdec_embed_rows", "qdec_rope_append_rows", "qdec_heads_to_rows_f16",
-           "qdec_swiglu_f16", "qattn_prefill_workspace_bytes", "qattn_prefill_rows_f16")
+           "qdec_swiglu_f16", "qattn_prefill_workspace_bytes", "qattn_prefill_rows_f16",
+           "qdec_argmax_rows_workspace_bytes", "qdec_argmax_rows", "qkv_plan", "qkv_rope_append",
+           "qattn_paged_workspace_bytes", "qattn_paged_f16")
 
 
 class QmError(RuntimeError):
@@ -103,6 +105,14 @@ def lib() -> ctypes.CDLL:
                                  vp, vp, vp, vp],
             "qdec_cast_f16": [vp, i64, vp, vp],
             "qdec_argmax": [vp, i64, vp, vp, sz, vp],
+            "qdec_argmax_rows_workspace_bytes": [i64, ctypes.POINTER(sz)],
+            "qdec_argmax_rows": [vp, i64, i64, vp, vp, sz, vp],
+            "qkv_plan": [vp, vp, i64, i32, vp, i64, i64, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp],
+            "qkv_rope_append": [vp, vp, vp, i32, i32, i32, i64, vp, vp, i32, vp, vp, ctypes.c_float, vp, i64, vp, vp,
+                                vp, i64, i32, vp],
+            "qattn_paged_workspace_bytes": [i32, i32, i32, i64, i64, i64, ctypes.POINTER(sz)],
+            "qattn_paged_f16": [vp, vp, vp, i64, i32, vp, i64, vp, i64, vp, vp, i64, i64, i32, i32, i32,
+                                ctypes.c_float, vp, vp, sz, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -594,6 +604,144 @@ def qdec_argmax(logits: torch.Tensor, out: Optional[torch.Tensor] = None, worksp
         workspace = torch.empty(ARGMAX_WORKSPACE_BYTES, dtype=torch.uint8, device=logits.device)
     _check(lib().qdec_argmax(_ptr(logits), logits.numel(), _ptr(out), _ptr(workspace), workspace.numel(),
                              _stream(stream)))
+    return out
+
+
+def qdec_argmax_rows_workspace_bytes(rows: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().qdec_argmax_rows_workspace_bytes(rows, ctypes.byref(b)))
+    return b.value
+
+
+def qdec_argmax_rows(logits: torch.Tensor, out: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, stream=None):
+    """fp32 [rows][n] -> int32 [rows] on the device (lowest index among equal maxima)."""
+    rows, n = logits.shape
+    _tensors(logits=(logits, torch.float32, (rows, n)))
+    if out is None:
+        out = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    if workspace is None:
+        workspace = torch.empty(qdec_argmax_rows_workspace_bytes(rows), dtype=torch.uint8, device=logits.device)
+    _tensors(out=(out, torch.int32, (rows,)), workspace=(workspace, torch.uint8, None))
+    _check(lib().qdec_argmax_rows(_ptr(logits), rows, n, _ptr(out), _ptr(workspace), workspace.numel(),
+                                  _stream(stream)))
+    return out
+
+
+def _tensors(**named) -> None:
+    """name=(tensor or None, type, shape or None).  Raises ValueError unless
+    every tensor has its type and shape (None: any), is contiguous and lies on
+    the current device, whose stream the call goes to."""
+    for name, (t, dtype, shape) in named.items():
+        if t is not None and (t.dtype != dtype or not t.is_contiguous() or (shape is not None and t.shape != shape)):
+            raise ValueError(f"{name}: need contiguous {dtype}{'' if shape is None else list(shape)}, got "
+                             f"{t.dtype}{list(t.shape)}{'' if t.is_contiguous() else ' (strided)'}")
+    here = torch.cuda.current_device()
+    for name, (t, _, _) in named.items():
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"{name}: on {t.device}, the current device is cuda:{here}")
+
+
+@dataclass
+class KvPlan:
+    """One step of a batch over a paged cache (qkv_plan's outputs)."""
+    lens: torch.Tensor        # int32 [n_req]: tokens held after the step (the next step's lens)
+    kv_lens: torch.Tensor     # int32 [n_req]: keys that the last token attends to
+    offsets: torch.Tensor     # int32 [n_req + 1]
+    positions: torch.Tensor   # int32 [max_tokens], -1: no token
+    slots: torch.Tensor       # int64 [max_tokens], -1: no token
+    ring: torch.Tensor        # int32 [2]: head and count of the free ring after the step
+    refused: torch.Tensor     # int32 [1]
+
+
+def empty_kv_plan(n_req: int, max_tokens: int, device="cuda") -> KvPlan:
+    def ints(n, dtype=torch.int32):
+        return torch.empty(n, dtype=dtype, device=device)
+    return KvPlan(ints(n_req), ints(n_req), ints(n_req + 1), ints(max_tokens), ints(max_tokens, torch.int64), ints(2),
+                  ints(1))
+
+
+def qkv_plan(lens: torch.Tensor, new_lens: torch.Tensor, tables: torch.Tensor, free_ring: torch.Tensor,
+             ring: torch.Tensor, page_size: int, max_tokens: int, prefix_pages: int = 0,
+             out: Optional[KvPlan] = None, stream=None) -> KvPlan:
+    """Page tables (in place), slots, positions and lengths of one step of a
+    batch; lens, new_lens int32 [n_req] (new_lens < 0: the request has ended),
+    tables int32 [n_req][max_pages], free_ring int32 [n_pages], ring int32 [2]."""
+    n_req, max_pages = tables.shape
+    i32 = torch.int32
+    if out is None:
+        out = empty_kv_plan(n_req, max_tokens, tables.device)
+    _tensors(lens=(lens, i32, (n_req,)), new_lens=(new_lens, i32, (n_req,)), tables=(tables, i32, None),
+             free_ring=(free_ring, i32, (free_ring.numel(),)), ring=(ring, i32, (2,)),
+             out_lens=(out.lens, i32, (n_req,)), out_kv_lens=(out.kv_lens, i32, (n_req,)),
+             out_offsets=(out.offsets, i32, (n_req + 1,)), out_positions=(out.positions, i32, (max_tokens,)),
+             out_slots=(out.slots, torch.int64, (max_tokens,)), out_ring=(out.ring, i32, (2,)),
+             out_refused=(out.refused, i32, (1,)))
+    _check(lib().qkv_plan(_ptr(lens), _ptr(new_lens), n_req, page_size, _ptr(tables), max_pages, prefix_pages,
+                          _ptr(free_ring), _ptr(ring), free_ring.numel(), max_tokens, _ptr(out.lens),
+                          _ptr(out.kv_lens), _ptr(out.offsets), _ptr(out.positions), _ptr(out.slots), _ptr(out.ring),
+                          _ptr(out.refused), _stream(stream)))
+    return out
+
+
+def qkv_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
+                    table: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, interleaved: bool = False,
+                    q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q fp32 [tokens][Hq*D], k, v fp32 [tokens][Hkv*D] -> fp16 [tokens][Hq][D];
+    keys and values into the pools fp16 [n_pages][Hkv][page][D] at the slots
+    (int64 [tokens]); table: qdec_rope_table's [positions][D/2][2]."""
+    n_pages, hkv, page, d = k_pages.shape
+    t = q.shape[0]
+    hq = q.shape[1] // d
+    f32, f16 = torch.float32, torch.float16
+    if q_out is None:
+        q_out = torch.empty((t, hq, d), dtype=f16, device=q.device)
+    _tensors(q=(q, f32, (t, hq * d)), k=(k, f32, (t, hkv * d)), v=(v, f32, (t, hkv * d)),
+             positions=(positions, torch.int32, (t,)), slots=(slots, torch.int64, (t,)),
+             table=(table, f32, (table.shape[0], d // 2, 2)), k_pages=(k_pages, f16, None),
+             v_pages=(v_pages, f16, k_pages.shape), q_norm=(q_norm, f16, (d,)), k_norm=(k_norm, f16, (d,)),
+             q_out=(q_out, f16, (t, hq, d)))
+    _check(lib().qkv_rope_append(_ptr(q), _ptr(k), _ptr(v), hq, hkv, d, t, _ptr(positions), _ptr(slots),
+                                 1 if interleaved else 0, _ptr(q_norm), _ptr(k_norm), eps, _ptr(table),
+                                 table.shape[0], _ptr(q_out), _ptr(k_pages), _ptr(v_pages), n_pages, page,
+                                 _stream(stream)))
+    return q_out
+
+
+def qattn_paged_workspace_bytes(n_q_heads: int, n_kv_heads: int, head_dim: int, n_req: int, tokens: int,
+                                prefix_pages: int = 0) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().qattn_paged_workspace_bytes(n_q_heads, n_kv_heads, head_dim, n_req, tokens, prefix_pages,
+                                             ctypes.byref(b)))
+    return b.value
+
+
+def qattn_paged_f16(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, tables: torch.Tensor,
+                    offsets: torch.Tensor, kv_lens: torch.Tensor, scale: float,
+                    prefix: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q fp16 [tokens][Hq][D]; pools fp16 [n_pages][Hkv][page][D]; tables int32
+    [n_req][max_pages]; offsets int32 [n_req + 1]; kv_lens int32 [n_req];
+    prefix: int32 [prefix_pages], the pages that all requests share ->
+    fp16 [tokens][Hq * D]."""
+    n_pages, hkv, page, d = k_pages.shape
+    t, hq, _ = q.shape
+    n_req, max_pages = tables.shape
+    f16, i32 = torch.float16, torch.int32
+    shared = 0 if prefix is None else prefix.numel()
+    if out is None:
+        out = torch.empty((t, hq * d), dtype=f16, device=q.device)
+    if workspace is None:
+        nb = qattn_paged_workspace_bytes(hq, hkv, d, n_req, t, shared)
+        workspace = torch.empty(max(nb, 16), dtype=torch.uint8, device=q.device)
+    _tensors(q=(q, f16, (t, hq, d)), k_pages=(k_pages, f16, None), v_pages=(v_pages, f16, k_pages.shape),
+             tables=(tables, i32, None), offsets=(offsets, i32, (n_req + 1,)), kv_lens=(kv_lens, i32, (n_req,)),
+             prefix=(prefix, i32, (shared,)), out=(out, f16, (t, hq * d)),
+             workspace=(workspace, torch.uint8, None))
+    _check(lib().qattn_paged_f16(_ptr(q), _ptr(k_pages), _ptr(v_pages), n_pages, page, _ptr(tables), max_pages,
+                                 _ptr(prefix) if shared else None, shared, _ptr(offsets), _ptr(kv_lens), n_req, t, hq,
+                                 hkv, d, scale, _ptr(out), _ptr(workspace), workspace.numel(), _stream(stream)))
     return out
 
 

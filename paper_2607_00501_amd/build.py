@@ -28,7 +28,8 @@ COMMON = [
 # overrides (for tuning sweeps only; the default build ignores them).
 if os.environ.get("QM_BUILD_TUNING") == "1":
     COMMON.append("-DQM_TUNING_OVERRIDES")
-SOURCES = ["api.cpp", "format.hip", "gemv.hip", "gemm.hip", "gemm_swiglu.hip", "fewrow.hip", "moe.hip", "attention.hip", "decode.hip"]
+SOURCES = ["api.cpp", "format.hip", "gemv.hip", "gemm.hip", "gemm_swiglu.hip", "fewrow.hip", "moe.hip", "attention.hip",
+           "paged_attention.hip", "kv_plan.hip", "decode.hip"]
 
 
 def _compile(src: str) -> str:

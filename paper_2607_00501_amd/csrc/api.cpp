@@ -759,7 +759,172 @@ qm_status qdec_argmax(const float* logits, int64_t n, int32_t* token, void* work
                 ws_bytes);
   if (!aligned4(logits) || !aligned4(token) || !aligned4(workspace))
     return fail(QM_EALIGN, "qdec_argmax: logits, token and workspace 4-byte aligned");
-  return launched(launch_argmax(logits, n, token, workspace, static_cast<hipStream_t>(stream)), "qdec_argmax");
+  return launched(launch_argmax(logits, 1, n, token, workspace, static_cast<hipStream_t>(stream)), "qdec_argmax");
+}
+
+qm_status qdec_argmax_rows_workspace_bytes(int64_t rows, size_t* bytes) {
+  if (!bytes) return fail(QM_EINVAL, "qdec_argmax_rows_workspace_bytes: null output pointer");
+  if (rows < 0 || rows > kArgmaxMaxRows)
+    return fail(QM_ESHAPE, "qdec_argmax_rows_workspace_bytes: rows must be in [0, %lld]", (long long)kArgmaxMaxRows);
+  *bytes = static_cast<size_t>(rows) * QDEC_ARGMAX_WORKSPACE_BYTES;
+  return QM_OK;
+}
+
+qm_status qdec_argmax_rows(const float* logits, int64_t rows, int64_t n, int32_t* tokens, void* workspace,
+                           size_t ws_bytes, void* stream) {
+  const char* name = "qdec_argmax_rows";
+  if (rows < 0 || rows > kArgmaxMaxRows || n < 1 || n > INT32_MAX - 1)
+    return fail(QM_ESHAPE, "%s: need 0 <= rows <= %lld and 1 <= n < 2^31-1", name, (long long)kArgmaxMaxRows);
+  if (rows == 0) return QM_OK;
+  if (!logits || !tokens) return fail(QM_EINVAL, "%s: null pointer", name);
+  const size_t need = static_cast<size_t>(rows) * QDEC_ARGMAX_WORKSPACE_BYTES;
+  if (!workspace || ws_bytes < need)
+    return fail(QM_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", name, need, workspace ? ws_bytes : 0);
+  if (!aligned4(logits) || !aligned4(tokens) || !aligned4(workspace))
+    return fail(QM_EALIGN, "%s: logits, tokens and workspace 4-byte aligned", name);
+  return launched(launch_argmax(logits, rows, n, tokens, workspace, static_cast<hipStream_t>(stream)), name);
+}
+
+// Page size, as its logarithm, and page count of a paged cache.
+static qm_status check_pages(const char* name, int32_t page_size, int64_t n_pages, int* page_log2) {
+  *page_log2 = 0;
+  while ((1 << *page_log2) < page_size && *page_log2 < 9) ++*page_log2;
+  if (page_size < 16 || page_size > 256 || (1 << *page_log2) != page_size)
+    return fail(QM_ESHAPE, "%s: page_size=%d must be 16, 32, 64, 128 or 256", name, page_size);
+  if (n_pages < 1 || n_pages > INT32_MAX)
+    return fail(QM_ESHAPE, "%s: n_pages=%lld must be in [1, 2^31)", name, (long long)n_pages);
+  return QM_OK;
+}
+
+// Requests, page table width and prefix of a batch.
+static qm_status check_batch(const char* name, int64_t n_req, int64_t max_pages, int64_t prefix_pages,
+                             int64_t max_tokens) {
+  if (n_req < 1 || n_req > kKvMaxRequests)
+    return fail(QM_ESHAPE, "%s: n_req=%lld must be in [1, %d]", name, (long long)n_req, kKvMaxRequests);
+  if (max_pages < 1 || max_pages > kKvMaxTablePages)
+    return fail(QM_ESHAPE, "%s: max_pages=%lld must be in [1, 2^20]", name, (long long)max_pages);
+  if (prefix_pages < 0 || prefix_pages > max_pages)
+    return fail(QM_ESHAPE, "%s: prefix_pages=%lld must be in [0, max_pages]", name, (long long)prefix_pages);
+  if (max_tokens < 0 || max_tokens > kKvMaxTokens)
+    return fail(QM_ESHAPE, "%s: tokens=%lld must be in [0, %lld]", name, (long long)max_tokens,
+                (long long)kKvMaxTokens);
+  return QM_OK;
+}
+
+qm_status qkv_plan(const int32_t* lens, const int32_t* new_lens, int64_t n_req, int32_t page_size, int32_t* tables,
+                   int64_t max_pages, int64_t prefix_pages, int32_t* free_ring, const int32_t* ring, int64_t n_pages,
+                   int64_t max_tokens, int32_t* lens_out, int32_t* kv_lens, int32_t* offsets, int32_t* positions,
+                   int64_t* slots, int32_t* ring_out, int32_t* refused, void* stream) {
+  const char* name = "qkv_plan";
+  KvPlanArgs a{};
+  qm_status st;
+  if ((st = check_pages(name, page_size, n_pages, &a.page_log2)) != QM_OK) return st;
+  if ((st = check_batch(name, n_req, max_pages, prefix_pages, max_tokens)) != QM_OK) return st;
+  if (!lens || !new_lens || !tables || !free_ring || !ring || !lens_out || !kv_lens || !offsets || !ring_out ||
+      !refused || (max_tokens > 0 && (!positions || !slots)))
+    return fail(QM_EINVAL, "%s: null pointer", name);
+  if (lens_out == lens || ring_out == ring)
+    return fail(QM_EINVAL, "%s: lens_out and ring_out must not be lens and ring (every workgroup reads those)", name);
+  const void* ints[] = {lens, new_lens, tables, free_ring, ring, lens_out, kv_lens, offsets, positions, ring_out, refused};
+  for (const void* p : ints)
+    if (!aligned4(p)) return fail(QM_EALIGN, "%s: pointers must be 4-byte aligned", name);
+  if (!aligned8(slots)) return fail(QM_EALIGN, "%s: slots must be 8-byte aligned", name);
+  a.lens = lens; a.new_lens = new_lens; a.tables = tables; a.free_ring = free_ring; a.ring = ring;
+  a.lens_out = lens_out; a.kv_lens = kv_lens; a.offsets = offsets; a.positions = positions; a.slots = slots;
+  a.ring_out = ring_out; a.refused = refused;
+  a.n_req = static_cast<int>(n_req); a.max_pages = static_cast<int>(max_pages);
+  a.n_pages = static_cast<int>(n_pages); a.prefix_pages = static_cast<int>(prefix_pages);
+  a.max_tokens = static_cast<int>(max_tokens);
+  return launched(launch_kv_plan(a, static_cast<hipStream_t>(stream)), name);
+}
+
+qm_status qkv_rope_append(const float* q, const float* k, const float* v, int32_t n_q_heads, int32_t n_kv_heads,
+                          int32_t head_dim, int64_t tokens, const int32_t* positions, const int64_t* slots,
+                          int32_t interleaved, const uint16_t* q_norm, const uint16_t* k_norm, float eps,
+                          const float* table, int64_t table_len, uint16_t* q_out, uint16_t* k_pages,
+                          uint16_t* v_pages, int64_t n_pages, int32_t page_size, void* stream) {
+  const char* name = "qkv_rope_append";
+  KvAppendArgs a{};
+  qm_status st;
+  if ((st = check_pages(name, page_size, n_pages, &a.page_log2)) != QM_OK) return st;
+  if (head_dim != 64 && head_dim != 128) return fail(QM_ESHAPE, "%s: head_dim=%d must be 64 or 128", name, head_dim);
+  if (n_q_heads < 1 || n_q_heads > 1024 || n_kv_heads < 1 || n_kv_heads > 1024)
+    return fail(QM_ESHAPE, "%s: head counts must be in [1, 1024]", name);
+  if (tokens < 0 || tokens > kKvMaxTokens)
+    return fail(QM_ESHAPE, "%s: tokens=%lld must be in [0, %lld]", name, (long long)tokens, (long long)kKvMaxTokens);
+  if (table_len < 1) return fail(QM_ESHAPE, "%s: the (cos, sin) table must have at least one position", name);
+  if (interleaved != 0 && interleaved != 1) return fail(QM_EINVAL, "%s: interleaved must be 0 or 1", name);
+  if ((q_norm == nullptr) != (k_norm == nullptr) || !aligned2(q_norm) || !aligned2(k_norm))
+    return fail(QM_EINVAL, "%s: q_norm and k_norm both given (2-byte aligned) or both NULL", name);
+  if (q_norm && (!(eps >= 0.0f) || eps == INFINITY)) return fail(QM_EINVAL, "%s: eps finite and >= 0", name);
+  if (tokens == 0) return QM_OK;
+  if (!q || !k || !v || !positions || !slots || !table || !q_out || !k_pages || !v_pages)
+    return fail(QM_EINVAL, "%s: null pointer", name);
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned8(q_out) || !aligned8(k_pages) || !aligned8(v_pages) ||
+      !aligned8(table) || !aligned8(slots) || !aligned4(positions))
+    return fail(QM_EALIGN, "%s: q, k, v 16-byte, q_out, pools, table and slots 8-byte, positions 4-byte aligned", name);
+  a.q = q; a.k = k; a.v = v; a.positions = positions; a.slots = slots;
+  a.table = reinterpret_cast<const float2*>(table); a.table_len = table_len;
+  a.q_gain = q_norm; a.k_gain = k_norm; a.eps = eps;
+  a.q_out = q_out; a.k_pages = k_pages; a.v_pages = v_pages; a.n_pages = n_pages;
+  a.tokens = static_cast<int>(tokens); a.hq = n_q_heads; a.hkv = n_kv_heads; a.interleaved = interleaved;
+  return launched(launch_rope_append_paged(a, head_dim, static_cast<hipStream_t>(stream)), name);
+}
+
+// Heads and sizes of a paged attention call.
+static qm_status check_paged_heads(const char* name, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (head_dim != 64 && head_dim != 128) return fail(QM_ESHAPE, "%s: head_dim=%d must be 64 or 128", name, head_dim);
+  if (n_kv_heads < 1 || n_kv_heads > 128 || n_q_heads < 1 || n_q_heads > 1024 || n_q_heads % n_kv_heads)
+    return fail(QM_ESHAPE, "%s: need n_kv_heads in [1, 128], n_q_heads in [1, 1024], a multiple of n_kv_heads", name);
+  return QM_OK;
+}
+
+qm_status qattn_paged_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t n_req,
+                                      int64_t tokens, int64_t prefix_pages, size_t* bytes) {
+  const char* name = "qattn_paged_workspace_bytes";
+  if (!bytes) return fail(QM_EINVAL, "%s: null output pointer", name);
+  qm_status st;
+  if ((st = check_paged_heads(name, n_q_heads, n_kv_heads, head_dim)) != QM_OK) return st;
+  if ((st = check_batch(name, n_req, kKvMaxTablePages, prefix_pages, tokens)) != QM_OK) return st;
+  const DeviceInfo* d;
+  if ((st = device_info(&d)) != QM_OK) return st;
+  *bytes = attn_paged_workspace_bytes(n_q_heads, n_kv_heads, head_dim, n_req, tokens, prefix_pages > 0, d->cu_count);
+  return QM_OK;
+}
+
+qm_status qattn_paged_f16(const uint16_t* q, const uint16_t* k_pages, const uint16_t* v_pages, int64_t n_pages,
+                          int32_t page_size, const int32_t* tables, int64_t max_pages, const int32_t* prefix,
+                          int64_t prefix_pages, const int32_t* offsets, const int32_t* kv_lens, int64_t n_req,
+                          int64_t tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                          uint16_t* out, void* workspace, size_t ws_bytes, void* stream) {
+  const char* name = "qattn_paged_f16";
+  PagedAttnArgs a{};
+  qm_status st;
+  if ((st = check_pages(name, page_size, n_pages, &a.page_log2)) != QM_OK) return st;
+  if ((st = check_batch(name, n_req, max_pages, prefix_pages, tokens)) != QM_OK) return st;
+  if ((st = check_paged_heads(name, n_q_heads, n_kv_heads, head_dim)) != QM_OK) return st;
+  if (!(scale > 0.0f) || scale == INFINITY) return fail(QM_EINVAL, "%s: scale must be finite and > 0", name);
+  if (tokens == 0) return QM_OK;
+  if (!q || !k_pages || !v_pages || !tables || !offsets || !kv_lens || !out || (prefix_pages > 0 && !prefix))
+    return fail(QM_EINVAL, "%s: null pointer", name);
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) || !aligned16(workspace))
+    return fail(QM_EALIGN, "%s: q, pools, out and workspace must be 16-byte aligned", name);
+  if (!aligned4(tables) || !aligned4(prefix) || !aligned4(offsets) || !aligned4(kv_lens))
+    return fail(QM_EALIGN, "%s: tables, prefix, offsets and kv_lens must be 4-byte aligned", name);
+  const DeviceInfo* d;
+  if ((st = device_info(&d)) != QM_OK) return st;
+  const size_t need =
+      attn_paged_workspace_bytes(n_q_heads, n_kv_heads, head_dim, n_req, tokens, prefix_pages > 0, d->cu_count);
+  if (!workspace || ws_bytes < need)
+    return fail(QM_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", name, need, workspace ? ws_bytes : 0);
+  a.q = q; a.k_pages = k_pages; a.v_pages = v_pages; a.tables = tables; a.prefix = prefix;
+  a.offsets = offsets; a.kv_lens = kv_lens; a.out = out; a.ws = static_cast<float*>(workspace);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.n_req = static_cast<int>(n_req); a.tokens = static_cast<int>(tokens);
+  a.hkv = n_kv_heads; a.group = n_q_heads / n_kv_heads;
+  a.max_pages = static_cast<int>(max_pages); a.n_pages = static_cast<int>(n_pages);
+  a.prefix_pages = static_cast<int>(prefix_pages);
+  return launched(launch_attn_paged(a, head_dim, ws_bytes, d->cu_count, static_cast<hipStream_t>(stream)), name);
 }
 
 qm_status qmoe_workspace_bytes(int64_t m, int32_t n_experts, int32_t top_k, int64_t hidden, int64_t inter,

@@ -269,33 +269,15 @@ __global__ void rope_append_rows_kernel(const float* __restrict__ q, const float
   dst[i + half] = f2h(rope_high(a, b, cs.x, cs.y));
 }
 
-// The same for a prompt chunk with a (cos, sin) table and aligned buffers: a
-// thread takes 4 pairs of one head (8 outputs) with 16-byte loads and 8-byte
-// stores, and workgroups of 256 threads run over (token, head, 4 pairs).  The
-// kernel above has half-empty wavefronts and 2-byte stores: 8.0 us for
-// 512 tokens of 32 + 2 x 8 heads of 64, 9 MB; this one 4.3 (64 tokens: 3.1, 2.9).  Each sum of a
-// head's squares is the kernel above's tree, so the results are the same bits.
+// Four pairs of one head from src (pairs i0 .. i0 + 3 of its D / 2), normed
+// (gain given), rotated by the (cos, sin) of row cs and rounded to dst; the D / 8
+// threads of a head are neighbours.  value: copied and rounded only.  Each sum of a
+// head's squares is the tree of the kernels above, so the results are the same bits.
 template <int D>
-__global__ __launch_bounds__(256) void rope_append_rows_vec_kernel(
-    const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v, int hq, int hkv, int m,
-    int64_t p0, int64_t max_len, int interleaved, uint16_t* __restrict__ q_out, uint16_t* __restrict__ kc,
-    uint16_t* __restrict__ vc, const uint16_t* __restrict__ q_gain, const uint16_t* __restrict__ k_gain, float eps,
-    const float2* __restrict__ table) {
+__device__ __forceinline__ void rope_head_vec(const float* __restrict__ src, uint16_t* __restrict__ dst,
+                                              const float2* __restrict__ cs_row, int i0, bool value, bool interleaved,
+                                              const uint16_t* __restrict__ gain, float eps) {
   constexpr int HALF = D / 2, T = D / 8;                  // threads per head
-  const int heads = hq + 2 * hkv;
-  const uint32_t e = blockIdx.x * 256u + threadIdx.x;     // < 32768 * 3072 * 16 + 256
-  const uint32_t unit = e / T;
-  const int i0 = 4 * static_cast<int>(e % T);             // first of the thread's four pairs
-  const int r = static_cast<int>(unit / heads), h = static_cast<int>(unit % heads);
-  if (r >= m) return;                                     // whole heads
-  const int64_t pos = p0 + r;
-  const bool value = h >= hq + hkv;
-  const float* src = h < hq  ? q + (static_cast<int64_t>(r) * hq + h) * D
-                     : value ? v + (static_cast<int64_t>(r) * hkv + (h - hq - hkv)) * D
-                             : k + (static_cast<int64_t>(r) * hkv + (h - hq)) * D;
-  uint16_t* dst = h < hq  ? q_out + (static_cast<int64_t>(h) * m + r) * D
-                  : value ? vc + (static_cast<int64_t>(h - hq - hkv) * max_len + pos) * D
-                          : kc + (static_cast<int64_t>(h - hq) * max_len + pos) * D;
   const bool pairs = interleaved && !value;               // columns 2i, 2i + 1 hold pair i
   const float4 u = *reinterpret_cast<const float4*>(src + (pairs ? 2 * i0 : i0));
   const float4 w = *reinterpret_cast<const float4*>(src + (pairs ? 2 * i0 + 4 : i0 + HALF));
@@ -316,9 +298,8 @@ __global__ __launch_bounds__(256) void rope_append_rows_vec_kernel(
   } else {
     float2 cs[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) cs[j] = table[pos * HALF + i0 + j];
-    if (q_gain) {
-      const uint16_t* gain = h < hq ? q_gain : k_gain;
+    for (int j = 0; j < 4; ++j) cs[j] = cs_row[i0 + j];
+    if (gain) {
       float ss[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -346,6 +327,63 @@ __global__ __launch_bounds__(256) void rope_append_rows_vec_kernel(
   *reinterpret_cast<uint2*>(dst + i0 + HALF) = make_uint2(hi[0], hi[1]);
 }
 
+// The same for a prompt chunk with a (cos, sin) table and aligned buffers: a
+// thread takes 4 pairs of one head (8 outputs) with 16-byte loads and 8-byte
+// stores, and workgroups of 256 threads run over (token, head, 4 pairs).  The
+// kernel above has half-empty wavefronts and 2-byte stores: 8.0 us for
+// 512 tokens of 32 + 2 x 8 heads of 64, 9 MB; this one 4.3 (64 tokens: 3.1, 2.9).
+template <int D>
+__global__ __launch_bounds__(256) void rope_append_rows_vec_kernel(
+    const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v, int hq, int hkv, int m,
+    int64_t p0, int64_t max_len, int interleaved, uint16_t* __restrict__ q_out, uint16_t* __restrict__ kc,
+    uint16_t* __restrict__ vc, const uint16_t* __restrict__ q_gain, const uint16_t* __restrict__ k_gain, float eps,
+    const float2* __restrict__ table) {
+  constexpr int HALF = D / 2, T = D / 8;                  // threads per head
+  const int heads = hq + 2 * hkv;
+  const uint32_t e = blockIdx.x * 256u + threadIdx.x;     // < 32768 * 3072 * 16 + 256
+  const uint32_t unit = e / T;
+  const int i0 = 4 * static_cast<int>(e % T);             // first of the thread's four pairs
+  const int r = static_cast<int>(unit / heads), h = static_cast<int>(unit % heads);
+  if (r >= m) return;                                     // whole heads
+  const int64_t pos = p0 + r;
+  const bool value = h >= hq + hkv;
+  const float* src = h < hq  ? q + (static_cast<int64_t>(r) * hq + h) * D
+                     : value ? v + (static_cast<int64_t>(r) * hkv + (h - hq - hkv)) * D
+                             : k + (static_cast<int64_t>(r) * hkv + (h - hq)) * D;
+  uint16_t* dst = h < hq  ? q_out + (static_cast<int64_t>(h) * m + r) * D
+                  : value ? vc + (static_cast<int64_t>(h - hq - hkv) * max_len + pos) * D
+                          : kc + (static_cast<int64_t>(h - hq) * max_len + pos) * D;
+  rope_head_vec<D>(src, dst, table + pos * HALF, i0, value, interleaved, q_gain ? (h < hq ? q_gain : k_gain) : nullptr,
+                   eps);
+}
+
+// The same for the tokens of a batch over a paged cache: token r has its own
+// position and slot, its queries go to row r of q_out, its keys and values to
+// row slot % page of page slot / page.  What bounds it is HBM, 6 bytes per
+// element.  A token without a position or a slot in the cache writes nothing.
+template <int D>
+__global__ __launch_bounds__(256) void rope_append_paged_kernel(KvAppendArgs p) {
+  constexpr int HALF = D / 2, T = D / 8;                  // threads per head
+  const int heads = p.hq + 2 * p.hkv;
+  const uint32_t e = blockIdx.x * 256u + threadIdx.x;     // < 65536 * 3072 * 16 + 256
+  const uint32_t unit = e / T;
+  const int i0 = 4 * static_cast<int>(e % T);             // first of the thread's four pairs
+  const int r = static_cast<int>(unit / heads), h = static_cast<int>(unit % heads);
+  if (r >= p.tokens) return;                              // whole heads
+  const int64_t slot = p.slots[r];
+  const int pos = p.positions[r];
+  if (slot < 0 || slot >> p.page_log2 >= p.n_pages || pos < 0 || pos >= p.table_len) return;   // whole heads
+  const bool value = h >= p.hq + p.hkv;
+  const int kh = value ? h - p.hq - p.hkv : h - p.hq;
+  const float* src = h < p.hq ? p.q + (static_cast<int64_t>(r) * p.hq + h) * D
+                              : (value ? p.v : p.k) + (static_cast<int64_t>(r) * p.hkv + kh) * D;
+  const int64_t row = slot & ((1 << p.page_log2) - 1), page = slot >> p.page_log2;
+  uint16_t* dst = h < p.hq ? p.q_out + (static_cast<int64_t>(r) * p.hq + h) * D
+                           : (value ? p.v_pages : p.k_pages) + (((page * p.hkv + kh) << p.page_log2) + row) * D;
+  rope_head_vec<D>(src, dst, p.table + static_cast<int64_t>(pos) * HALF, i0, value, p.interleaved,
+                   p.q_gain ? (h < p.hq ? p.q_gain : p.k_gain) : nullptr, p.eps);
+}
+
 // o [H][m][D] fp32 -> out [m][H * D] fp16 (the output projection's input).
 __global__ __launch_bounds__(256) void heads_to_rows_kernel(const float* __restrict__ o, int h, int64_t m, int d,
                                                             uint16_t* __restrict__ out) {
@@ -370,9 +408,9 @@ __global__ __launch_bounds__(256) void cast_f16_kernel(const float* __restrict__
   for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) y[i] = f2h(x[i]);
 }
 
-// Greedy sampling: index of the largest logit, the lowest index among equal
-// ones; NaNs are never chosen; 0 if every logit is NaN.  Pass 1: each of up
-// to kArgmaxBlocks workgroups reduces a strided share of the logits, four
+// Greedy sampling: index of the largest logit of each row (grid y), the lowest
+// index among equal ones; NaNs are never chosen; 0 if every logit is NaN.  Pass
+// 1: each of up to kArgmaxBlocks workgroups reduces a strided share of a row, four
 // independent loads in flight per lane, to one (value, index) pair (a lone
 // workgroup writes the token directly); pass 2 reduces the pairs.
 constexpr int kArgmaxBlocks = 256;
@@ -406,6 +444,7 @@ __global__ __launch_bounds__(256) void argmax_partial_kernel(const float* __rest
                                                              int32_t* __restrict__ token) {
   float best = -INFINITY;
   int32_t idx = INT32_MAX;
+  x += blockIdx.y * n;
   const int64_t stride = static_cast<int64_t>(gridDim.x) * 256;
   for (int64_t base = blockIdx.x * 256 + threadIdx.x; base < n; base += 4 * stride) {
     float v[4];
@@ -425,10 +464,10 @@ __global__ __launch_bounds__(256) void argmax_partial_kernel(const float* __rest
   block_best(best, idx);
   if (threadIdx.x == 0) {
     if (gridDim.x == 1) {
-      token[0] = idx == INT32_MAX ? 0 : idx;
+      token[blockIdx.y] = idx == INT32_MAX ? 0 : idx;
     } else {
-      pv[blockIdx.x] = best;
-      pi[blockIdx.x] = idx;
+      pv[blockIdx.y * kArgmaxBlocks + blockIdx.x] = best;
+      pi[blockIdx.y * kArgmaxBlocks + blockIdx.x] = idx;
     }
   }
 }
@@ -439,11 +478,11 @@ __global__ __launch_bounds__(256) void argmax_final_kernel(const float* __restri
   float best = -INFINITY;
   int32_t idx = INT32_MAX;
   if (static_cast<int>(threadIdx.x) < nb) {
-    best = pv[threadIdx.x];
-    idx = pi[threadIdx.x];
+    best = pv[blockIdx.y * kArgmaxBlocks + threadIdx.x];
+    idx = pi[blockIdx.y * kArgmaxBlocks + threadIdx.x];
   }
   block_best(best, idx);
-  if (threadIdx.x == 0) token[0] = idx == INT32_MAX ? 0 : idx;
+  if (threadIdx.x == 0) token[blockIdx.y] = idx == INT32_MAX ? 0 : idx;
 }
 
 unsigned spread_blocks(int64_t n) {
@@ -571,16 +610,28 @@ hipError_t launch_cast_f16(const float* x, int64_t n, uint16_t* y, hipStream_t s
   return hipGetLastError();
 }
 
-hipError_t launch_argmax(const float* x, int64_t n, int32_t* token, void* ws, hipStream_t st) {
+hipError_t launch_rope_append_paged(const KvAppendArgs& p, int32_t d, hipStream_t st) {
+  if (p.tokens == 0) return hipSuccess;
+  const int64_t threads = p.tokens * (p.hq + 2 * static_cast<int64_t>(p.hkv)) * (d / 8);
+  const dim3 grid(static_cast<unsigned>((threads + 255) / 256));
+  if (d == 64)
+    hipLaunchKernelGGL(rope_append_paged_kernel<64>, grid, dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL(rope_append_paged_kernel<128>, grid, dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_argmax(const float* x, int64_t rows, int64_t n, int32_t* token, void* ws, hipStream_t st) {
   const int64_t want = (n + 4095) / 4096;
   const int nb = static_cast<int>(want < kArgmaxBlocks ? want : kArgmaxBlocks);
   float* pv = static_cast<float*>(ws);
-  int32_t* pi = reinterpret_cast<int32_t*>(pv + kArgmaxBlocks);
-  hipLaunchKernelGGL(argmax_partial_kernel, dim3(nb), dim3(256), 0, st, x, n, pv, pi, token);
+  int32_t* pi = reinterpret_cast<int32_t*>(pv + rows * kArgmaxBlocks);
+  const unsigned r = static_cast<unsigned>(rows);
+  hipLaunchKernelGGL(argmax_partial_kernel, dim3(nb, r), dim3(256), 0, st, x, n, pv, pi, token);
   if (nb == 1) return hipGetLastError();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(argmax_final_kernel, dim3(1), dim3(256), 0, st, pv, pi, nb, token);
+  hipLaunchKernelGGL(argmax_final_kernel, dim3(1, r), dim3(256), 0, st, pv, pi, nb, token);
   return hipGetLastError();
 }
 

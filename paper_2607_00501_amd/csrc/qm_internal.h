@@ -212,7 +212,53 @@ struct QkvRopeEpi {
 };
 hipError_t launch_gemv_qkv_norm_rope(int32_t fmt, GemvGroup& g, const NormArgs& na, const QkvRopeEpi& epi,
                                      int64_t k, int cu_count, hipStream_t st);
-hipError_t launch_argmax(const float* x, int64_t n, int32_t* token, void* ws, hipStream_t st);
+hipError_t launch_argmax(const float* x, int64_t rows, int64_t n, int32_t* token, void* ws, hipStream_t st);
+
+// Batched serving over a paged KV cache: pools fp16 [n_pages][hkv][page][d].
+constexpr int64_t kArgmaxMaxRows = 32768;
+constexpr int kKvMaxRequests = 1024;
+constexpr int64_t kKvMaxTokens = 65536;                 // of one step
+constexpr int64_t kKvMaxTablePages = int64_t{1} << 20;  // of one request: its tokens stay below 2^28
+
+struct KvPlanArgs {
+  const int32_t* lens; const int32_t* new_lens;   // [n_req]
+  int32_t* tables;                                // [n_req][max_pages]
+  int32_t* free_ring; const int32_t* ring;        // [n_pages]; head and count
+  int32_t* lens_out; int32_t* kv_lens;            // [n_req]
+  int32_t* offsets;                               // [n_req + 1]
+  int32_t* positions; int64_t* slots;             // [max_tokens]
+  int32_t* ring_out; int32_t* refused;            // [2], [1]
+  int n_req, page_log2, max_pages, n_pages, prefix_pages, max_tokens;
+};
+hipError_t launch_kv_plan(const KvPlanArgs& a, hipStream_t st);
+
+struct KvAppendArgs {
+  const float* q; const float* k; const float* v;                // [tokens][heads * d]
+  const int32_t* positions; const int64_t* slots;                // [tokens]
+  const float2* table; int64_t table_len;                        // (cos, sin) [table_len][d / 2]
+  const uint16_t* q_gain; const uint16_t* k_gain; float eps;
+  uint16_t* q_out; uint16_t* k_pages; uint16_t* v_pages;
+  int64_t n_pages;
+  int tokens, hq, hkv, page_log2, interleaved;
+};
+hipError_t launch_rope_append_paged(const KvAppendArgs& p, int32_t d, hipStream_t st);
+
+struct PagedAttnArgs {
+  const uint16_t* q;                              // [tokens][hkv * group][d]
+  const uint16_t* k_pages; const uint16_t* v_pages;
+  const int32_t* tables;                          // [n_req][max_pages]
+  const int32_t* prefix;                          // [prefix_pages]
+  const int32_t* offsets; const int32_t* kv_lens; // [n_req + 1], [n_req]
+  uint16_t* out;                                  // [tokens][hkv * group * d]
+  float* ws;
+  float scale_log2;
+  int n_req, tokens, hkv, group, page_log2, max_pages, n_pages, prefix_pages;
+  int target;                                     // workgroups per KV head that the keys are split for
+  int granules;                                   // 16-row granules that the workspace holds
+};
+size_t attn_paged_workspace_bytes(int32_t hq, int32_t hkv, int32_t d, int64_t n_req, int64_t tokens, bool prefix,
+                                  int cu_count);
+hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, size_t ws_bytes, int cu_count, hipStream_t st);
 
 struct MoeArgs {
   const uint8_t* gq; const uint16_t* gs;   // gate [E][inter][hidden], device layout
