@@ -21,6 +21,7 @@
 // every workgroup works it out by itself with two sums over the requests, so
 // the call needs no host copy of the lengths, no plan made before it, and can be
 // replayed from a graph while the lengths move on.
+#include "lds_dma.h"
 #include "qm_internal.h"
 
 #include <algorithm>
@@ -34,10 +35,16 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 
 constexpr int kBlockKeys = 64;      // keys are split in multiples of this
 constexpr int kMinBlocks = 2;       // fewest blocks of a split
-constexpr int kTile = 16;           // rows of a tile
-// Weights go to fp16 as 2^15 w: the largest is 32,768, and relative to it weights
-// keep 11 bits down to 2^-29 (2^-14 unscaled).  Sums of weights carry the same factor.
-constexpr float kWeightBits = 15.0f;
+// Rows of a tile: 16 where a request (or the whole batch, for the prefix) has no
+// more, else 128.  The four wavefronts of a workgroup share the rows of the first
+// and split its keys, and split the rows of the second and share its keys.
+constexpr int kNarrow = 16, kWide = 128;
+__host__ __device__ __forceinline__ int tile_rows(int rows) { return rows <= kNarrow ? kNarrow : kWide; }
+// A row's maximum moves only when it grows by more than 2^8, so that the sums are
+// rarely rescaled.  Weights go to fp16 as 2^7 w relative to it: the largest is
+// 2^15, and they keep 11 bits down to 2^-21.  Sums of values and of (rounded)
+// weights carry the same factor.
+constexpr float kWeightBits = 7.0f, kMaxSlack = 8.0f;
 
 // ------------------------------------------------------------ work units
 
@@ -67,29 +74,30 @@ __device__ __forceinline__ int request_of(const Requests& r, int n, int token) {
   return lo;
 }
 
-struct Share { int tiles, blocks, splits, granules; };   // of one request: granules per split of a tile
-
-__device__ __forceinline__ int rows_of(const Requests& r, const PagedAttnArgs& a, int i) {
-  return max(r.off[i + 1] - r.off[i], 0) * a.group;
-}
+struct Share {
+  int rows, tiles, blocks, splits;
+  int granules;   // of 16 rows, that a tile leaves in the workspace; 0: its only part writes the output itself
+};
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // c: blocks per split (0: not known yet).
 __device__ __forceinline__ Share share_of(const Requests& r, const PagedAttnArgs& a, int i, int c) {
-  const int rows = rows_of(r, a, i), own = r.kv[i] - (a.prefix_pages << a.page_log2);
+  const int own = r.kv[i] - (a.prefix_pages << a.page_log2);
   Share s;
-  s.tiles = (rows + kTile - 1) / kTile;
+  s.rows = max(r.off[i + 1] - r.off[i], 0) * a.group;
+  const int per = tile_rows(s.rows);
+  s.tiles = (s.rows + per - 1) / per;
   s.blocks = own > 0 ? (own + kBlockKeys - 1) / kBlockKeys : 1;
   s.splits = c ? ceil_div(s.blocks, c) : 1;
-  s.granules = s.splits > 1 || a.prefix_pages ? kTile / 16 : 0;   // a lone part writes the output itself
+  s.granules = s.splits > 1 || a.prefix_pages ? per / 16 : 0;
   return s;
 }
 
 // Every lane of a wavefront takes `per` consecutive requests; units_before and
 // granules_before are the sums over the earlier lanes' requests.
 struct Units {
-  int c, per, prefix_tiles, prefix_blocks, prefix_splits, units_before, granules_before, total;
+  int c, per, prefix_tile, prefix_tiles, prefix_splits, units_before, granules_before, total;
 };
 
 template <class T>
@@ -114,12 +122,14 @@ __device__ __forceinline__ Units make_units(const Requests& r, const PagedAttnAr
     work += static_cast<int64_t>(s.tiles) * s.blocks;
   }
   work = __shfl(wave_scan(work), 63);
-  u.prefix_blocks = ((a.prefix_pages << a.page_log2) + kBlockKeys - 1) / kBlockKeys;
-  u.prefix_tiles = a.prefix_pages ? (r.off[a.n_req] * a.group + kTile - 1) / kTile : 0;
-  work += static_cast<int64_t>(u.prefix_tiles) * u.prefix_blocks;
+  const int prefix_blocks = ((a.prefix_pages << a.page_log2) + kBlockKeys - 1) / kBlockKeys;
+  const int rows = r.off[a.n_req] * a.group;
+  u.prefix_tile = tile_rows(rows);
+  u.prefix_tiles = a.prefix_pages ? ceil_div(rows, u.prefix_tile) : 0;
+  work += static_cast<int64_t>(u.prefix_tiles) * prefix_blocks;
   // Splits of c blocks: sum tiles ceil(blocks / c) <= tiles + target.
   u.c = static_cast<int>(max<int64_t>(kMinBlocks, (work + a.target - 1) / a.target));
-  u.prefix_splits = a.prefix_pages ? ceil_div(u.prefix_blocks, u.c) : 0;
+  u.prefix_splits = a.prefix_pages ? ceil_div(prefix_blocks, u.c) : 0;
   int units = 0, granules = 0;
   for (int i = lo; i < hi; ++i) {
     const Share s = share_of(r, a, i, u.c);
@@ -129,14 +139,14 @@ __device__ __forceinline__ Units make_units(const Requests& r, const PagedAttnAr
   const int units_to = wave_scan(units), granules_to = wave_scan(granules);
   const int p = u.prefix_tiles * u.prefix_splits;
   u.units_before = p + units_to - units;
-  u.granules_before = p * (kTile / 16) + granules_to - granules;
+  u.granules_before = p * (u.prefix_tile / 16) + granules_to - granules;
   u.total = p + __shfl(units_to, 63);
   return u;
 }
 
 // ---------------------------------------------------- one part of one tile
 
-// Sixteen consecutive keys of a page table: where they lie.
+// A range of keys behind a page table.
 struct Keys {
   const int32_t* pages;   // page ids of positions 0, page, 2 page, ...
   int lo, hi;             // this part's keys: positions [lo, hi); lo is a multiple of 16
@@ -162,28 +172,48 @@ __device__ __forceinline__ half8v finite_part(half8v v, bool& seen) {
   return __builtin_bit_cast(half8v, w);
 }
 
+// Sum of the weights of a pair, as rounded, on top of l.
+__device__ __forceinline__ float add_pair(half8v w, int i, float l) {
+  const half2v one = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
+  return __builtin_amdgcn_fdot2(half2v{w[i], w[i + 1]}, one, l, false);
+}
+
 __device__ __forceinline__ half4v read_tr(const _Float16* p) {
   typedef __attribute__((address_space(3))) short4v* lds_ptr;
   return __builtin_bit_cast(half4v, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                         (lds_ptr)(const_cast<short4v*>(reinterpret_cast<const short4v*>(p)))));
 }
 
-// V in LDS: rows of D halves, the 16-byte chunk c of row r at chunk c ^ swizzle(r):
-// the four rows x 32 bytes that a group of 16 lanes reads transposed fall on
-// different banks.
+// K and V in LDS: rows of D halves, the 16-byte chunk c of row r at chunk
+// c ^ swizzle(r).  K is read as 16 bytes of 32 rows at once: eight lanes, on rows
+// one after the other, fall on different banks.  V is read transposed, four rows x
+// 32 bytes by 16 lanes: they do with twice the row.
+template <int D>
+__device__ __forceinline__ constexpr int k_swizzle(int row) { return row & (D / 8 - 1); }
+template <int D>
+__device__ __forceinline__ constexpr int v_swizzle(int row) { return (2 * row) & (D / 8 - 1); }
 template <int D>
 __device__ __forceinline__ int v_at(int row, int dim) {
-  constexpr int C = D / 8;
-  return row * D + (((dim >> 3) ^ ((2 * row) & (C - 1))) << 3) + (dim & 7);
+  return row * D + (((dim >> 3) ^ v_swizzle<D>(row)) << 3) + (dim & 7);
 }
 
 template <int D>
-struct TileLds {
+struct NarrowLds {
   union {
     _Float16 v[4][32 * D];          // a block of V per wavefront
     float acc[4][16][D + 4];        // the wavefronts' parts
   };
   float m[4][16], l[4][16];
+};
+template <int D>
+struct WideLds {
+  _Float16 k[2][kBlockKeys * D], v[2][kBlockKeys * D];   // two blocks: one read, one on its way
+  int bad;
+};
+template <int D>
+union TileLds {
+  NarrowLds<D> n;
+  WideLds<D> w;
 };
 
 // One tile of 16 rows against the keys [k.lo, k.hi) of one KV head: the four
@@ -194,8 +224,8 @@ struct TileLds {
 // limit: keys visible to this lane's row (lane & 15), 0 for rows that do not
 // exist.  Leaves the joined sums in s.acc[0], maxima in s.m[0], sums in s.l[0].
 template <int D>
-__device__ __forceinline__ void tile_part(const PagedAttnArgs& a, TileLds<D>& s, const uint16_t* q_row, int limit,
-                                          int head, const Keys& k) {
+__device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, NarrowLds<D>& s, const uint16_t* q_row, int limit,
+                                            int head, const Keys& k) {
   constexpr int KS = D / 32, DB = D / 16, VL = D / 16;   // k steps of S, dimension tiles, V loads per lane
   const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -278,22 +308,21 @@ __device__ __forceinline__ void tile_part(const PagedAttnArgs& a, TileLds<D>& s,
                      fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3])));
     bm = fmaxf(bm, __shfl_xor(bm, 16));
     bm = fmaxf(bm, __shfl_xor(bm, 32));
-    const float mn = fmaxf(m, bm * a.scale_log2);
+    const float mn = bm * a.scale_log2 > m + kMaxSlack ? bm * a.scale_log2 : m;
     const float alpha = __builtin_amdgcn_exp2f(m - mn);
     m = mn;
     half8v w;
-    float sum = 0.0f;
+    l *= alpha;                                             // of this lane's keys; joined at the end
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 4; r += 2) {
         const float w0 = __builtin_amdgcn_exp2f(fmaf(st[t][r], a.scale_log2, kWeightBits - mn));
         const float w1 = __builtin_amdgcn_exp2f(fmaf(st[t][r + 1], a.scale_log2, kWeightBits - mn));
-        sum += w0 + w1;
         w[4 * t + r] = static_cast<_Float16>(w0);           // to nearest: errors of the weights average out
         w[4 * t + r + 1] = static_cast<_Float16>(w1);
+        l = add_pair(w, 4 * t + r, l);
       }
-    l = fmaf(l, alpha, sum);                                // of this lane's keys; joined at the end
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
 #pragma unroll
       for (int b = 0; b < DB; ++b)
@@ -345,26 +374,200 @@ __device__ __forceinline__ void tile_part(const PagedAttnArgs& a, TileLds<D>& s,
   __syncthreads();
 }
 
+// One tile of 128 rows against the keys [k.lo, hi) of one KV head: wavefront w has
+// rows 32 w .. 32 w + 31, and all share the blocks of 64 keys that come into LDS by
+// DMA, each wavefront copying 16 keys of K and V, while the block before is worked on.
+//   S^T = K Q^T   32 keys x 32 rows at a time, K fragments out of LDS,
+//   O^T += V^T W^T as in narrow_part.
+// limit: keys visible to this lane's row (lane & 31).  acc[b][r]: dimension
+// 32 b + 8 (r / 4) + 4 (lane / 32) + r % 4 of the row; m, l: its maximum and this
+// lane's share of the sum of weights.
+template <int D>
+__device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s, const uint16_t* q_row, int limit,
+                                          int head, const Keys& k, float16v (&acc)[D / 32], float& m, float& l) {
+  constexpr int KS = D / 16, DB = D / 32, C = D / 8, PIECES = D / 32;   // PIECES: KiB of 16 keys
+  const int lane = threadIdx.x & 63, col = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int page_rows = 1 << a.page_log2, hi = k.hi;
+  int most = limit, least = limit > 0 ? limit : INT32_MAX;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    most = max(most, __shfl_xor(most, o));
+    least = min(least, __shfl_xor(least, o));
+  }
+  most = __builtin_amdgcn_readfirstlane(min(most, hi));             // nothing for this wavefront from here on
+  const int all = __builtin_amdgcn_readfirstlane(min(least, hi));   // keys below are visible to every row
+  half8v qf[KS];
+#pragma unroll
+  for (int c = 0; c < KS; ++c) qf[c] = *reinterpret_cast<const half8v*>(q_row + 16 * c + 8 * lh);
+  if (threadIdx.x == 0) s.bad = 0;
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[b][r] = 0.0f;
+  m = -FLT_MAX;
+  l = 0.0f;
+
+  // This wavefront's 16 keys of the block at kb (keys past the end: the last ones).
+  const int last = (hi - 1) & ~15;
+  bool bad = false;
+  auto page_of = [&](int kb) __attribute__((always_inline)) {
+    return __builtin_amdgcn_readfirstlane(k.pages[min(kb + 16 * wave, last) >> a.page_log2]);
+  };
+  const int lrow = lane / C, chunk = lane % C;            // of a piece: 64 / C rows of C chunks
+  auto copy = [&](int buf, int kb, int id) __attribute__((always_inline)) {
+    if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(a.n_pages)) {
+      bad = true;
+      id = 0;
+    }
+    const int t = min(kb + 16 * wave, last) & (page_rows - 1);
+    const int64_t row = ((static_cast<int64_t>(id) * a.hkv + head) << a.page_log2) + t;
+    const uint16_t* kr = a.k_pages + row * D;
+    const uint16_t* vr = a.v_pages + row * D;
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) {
+      const int r = j * (64 / C) + lrow;
+      qg::lds_dma16(kr + r * D + ((chunk ^ k_swizzle<D>(r)) << 3), &s.k[buf][16 * wave * D + 512 * j]);
+      qg::lds_dma16(vr + r * D + ((chunk ^ v_swizzle<D>(r)) << 3), &s.v[buf][16 * wave * D + 512 * j]);
+    }
+  };
+  auto compute = [&](int buf, int kb) __attribute__((always_inline)) {
+    const _Float16* const kl = s.k[buf];
+    const _Float16* const vl = s.v[buf];
+    float16v st[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[t][r] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < KS; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const half8v f =
+            *reinterpret_cast<const half8v*>(&kl[(32 * t + col) * D + (((2 * c + lh) ^ k_swizzle<D>(col)) << 3)]);
+        st[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, qf[c], st[t], 0, 0, 0);
+      }
+    // Lane: row col, keys kb + 32 t + 8 (r / 4) + 4 lh + r % 4.
+    const bool masked = kb + kBlockKeys > all;
+    if (masked) {
+      const int seen = min(limit, hi) - kb - 4 * lh;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st[t][r] = 32 * t + 8 * (r >> 2) + (r & 3) < seen ? st[t][r] : -INFINITY;
+    }
+    float bm = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) bm = fmaxf(bm, st[t][r]);
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
+    bm = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale_log2;
+    const float mn = bm > m + kMaxSlack ? bm : m;
+    if (__builtin_amdgcn_ballot_w64(mn != m) != 0) {
+      const float alpha = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[b][r] *= alpha;
+    }
+    const float shift = kWeightBits - m;
+    half8v w[4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        half8v& x = w[2 * t + (r >> 3)];
+        x[r & 7] = static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(st[t][r], a.scale_log2, shift)));
+        x[(r & 7) + 1] = static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(st[t][r + 1], a.scale_log2, shift)));
+        l = add_pair(x, r & 7, l);
+      }
+    // k slot (lh, j) of step kk: key 16 kk + 8 (j / 4) + 4 lh + j % 4.
+    auto value = [&](int kk, int b) __attribute__((always_inline)) {
+      const int row = 16 * kk + 4 * lh + ((lane & 15) >> 2), dim = 32 * b + (col & 16) + 4 * (lane & 3);
+      const half4v lo = read_tr(&vl[v_at<D>(row, dim)]);
+      const half4v up = read_tr(&vl[v_at<D>(row + 8, dim)]);
+      return half8v{lo[0], lo[1], lo[2], lo[3], up[0], up[1], up[2], up[3]};
+    };
+    if (!masked) {
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+          acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(kk, b), w[kk], acc[b], 0, 0, 0);
+    } else {                                                // as in narrow_part
+      bool odd = false;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+          acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(finite_part(value(kk, b), odd), w[kk], acc[b], 0, 0, 0);
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+        for (int key = 0; key < kBlockKeys; ++key) {
+          if (kb + key < min(limit, hi)) {
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const float x = static_cast<float>(vl[v_at<D>(key, 32 * b + 8 * (r >> 2) + 4 * lh + (r & 3))]);
+                acc[b][r] += __builtin_fabsf(x) < INFINITY ? 0.0f : x;
+              }
+          }
+        }
+      }
+    }
+  };
+  if (k.lo < hi) {
+    copy(0, k.lo, page_of(k.lo));
+    int id = page_of(k.lo + kBlockKeys);
+    int buf = 0;
+    for (int kb = k.lo; kb < hi; kb += kBlockKeys, buf ^= 1) {
+      // This wavefront's copies have landed and its reads of the other block are
+      // done; after the barrier so are everybody's.
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0xC07F);                   // lgkmcnt(0)
+      qg::vm_wait<0>();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (kb + kBlockKeys < hi) {
+        copy(buf ^ 1, kb + kBlockKeys, id);
+        id = page_of(kb + 2 * kBlockKeys);
+      }
+      if (kb < most) compute(buf, kb);
+    }
+  }
+  __syncthreads();
+  if (bad) s.bad = 1;
+  __syncthreads();
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+  if (s.bad) l = __builtin_nanf("");
+}
+
 template <int D>
 __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnArgs a) {
   __shared__ Requests req;
-  __shared__ TileLds<D> s;
+  __shared__ __attribute__((aligned(1024))) TileLds<D> s;
   load_requests(req, a);
   const Units u = make_units(req, a);
   const int head = static_cast<int>(blockIdx.x % a.hkv);
   const int unit = static_cast<int>(blockIdx.x / a.hkv);
   if (unit >= u.total) return;
   const int prefix_len = a.prefix_pages << a.page_log2;
-  const int lane = threadIdx.x & 63, col = lane & 15;
-  int row0, rows, part, granule, i = 0;                     // first row of the tile, counted over the batch or the request
+  const int lane = threadIdx.x & 63;
+  int row0, rows, per, granule, i = 0;                      // tile: first row, counted over the batch or the request
   Keys k;
   bool direct = false;
-  const int p = u.prefix_tiles * u.prefix_splits;
-  if (unit < p) {
-    row0 = unit / u.prefix_splits * kTile;
+  const bool shared = unit < u.prefix_tiles * u.prefix_splits;
+  // Parts of the same keys follow each other: they share what the L2 holds.
+  if (shared) {
+    per = u.prefix_tile;
+    row0 = unit % u.prefix_tiles * per;
     rows = req.off[a.n_req] * a.group;
-    part = unit % u.prefix_splits;
-    granule = unit * (kTile / 16);
+    const int part = unit / u.prefix_tiles;
+    granule = unit * (per / 16);
     k = Keys{a.prefix, part * u.c * kBlockKeys, min(prefix_len, (part + 1) * u.c * kBlockKeys)};
   } else {
     // The lane whose requests hold the unit, then the request.
@@ -380,47 +583,81 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnArgs a) {
       granule += sh.tiles * sh.splits * sh.granules;
       sh = share_of(req, a, ++i, u.c);
     }
-    const int tile = (unit - at) / sh.splits;
-    part = (unit - at) % sh.splits;
+    rows = sh.rows;
+    per = tile_rows(rows);
+    row0 = (unit - at) % sh.tiles * per;
+    const int part = (unit - at) / sh.tiles;
     granule += (unit - at) * sh.granules;
     direct = sh.granules == 0;
-    row0 = tile * kTile;
-    rows = rows_of(req, a, i);
     // Splits past the keys that the tile's last row sees have nothing to do
     // (the first is always there, so that every row is written).
-    const int last = min(row0 + kTile, rows) - 1;
-    const int seen = req.kv[i] - rows / a.group + last / a.group + 1 - prefix_len;
-    if (part > 0 && part * u.c * kBlockKeys >= seen) return;
+    const int last = min(row0 + per, rows) - 1;
+    const int seen = req.kv[i] - rows / a.group + last / a.group + 1;
     const int64_t lo = prefix_len + static_cast<int64_t>(part) * u.c * kBlockKeys;
+    if (part > 0 && lo >= seen) return;
     k = Keys{a.tables + static_cast<int64_t>(i) * a.max_pages, static_cast<int>(lo),
-             static_cast<int>(min<int64_t>(req.kv[i], lo + static_cast<int64_t>(u.c) * kBlockKeys))};
+             static_cast<int>(min<int64_t>(min(req.kv[i], seen), lo + static_cast<int64_t>(u.c) * kBlockKeys))};
   }
-  if (!direct && granule + kTile / 16 > a.granules) return;   // (the workspace covers every batch of these limits)
-  // This lane's row.
+  if (!direct && granule + per / 16 > a.granules) return;   // (the workspace covers every batch of these limits)
+  // This lane's row of the tile.
+  const bool narrow = per == kNarrow;
+  const int col = narrow ? lane & 15 : static_cast<int>(threadIdx.x >> 6) * 32 + (lane & 31);
   const int row = min(row0 + col, rows - 1);
   int token = row / a.group;
   const int gq = row % a.group;
-  if (unit < p) i = request_of(req, a.n_req, token);
+  if (shared) i = request_of(req, a.n_req, token);
   else token += req.off[i];
   const int j = token - req.off[i], t = max(req.off[i + 1] - req.off[i], 0);
-  int limit = max(min(req.kv[i] - t + j + 1, req.kv[i]), 0);
-  if (unit < p) limit = min(limit, prefix_len);
-  if (row0 + col >= rows) limit = 0;
+  const int sees = max(min(req.kv[i] - t + j + 1, req.kv[i]), 0);
+  const int limit = row0 + col >= rows ? 0 : shared ? min(sees, prefix_len) : sees;
   const int64_t hq = static_cast<int64_t>(a.hkv) * a.group;
-  const uint16_t* q_row = a.q + (static_cast<int64_t>(token) * hq + head * a.group + gq) * D;
-  tile_part<D>(a, s, q_row, limit, head, k);
+  const int64_t at_row = static_cast<int64_t>(token) * hq + head * a.group + gq;   // of q and out
+  if (!narrow) {
+    float16v acc[D / 32];
+    float m, l;
+    wide_part<D>(a, s.w, a.q + at_row * D, limit, head, k, acc, m, l);
+    if (row0 + col >= rows) return;
+    const int lh = lane >> 5;
+    if (direct) {
+      const float inv = sees ? 1.0f / l : 0.0f;
+      uint16_t* o = a.out + at_row * D;
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          half4v h;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(sees ? acc[b][r + c] * inv : 0.0f);
+          *reinterpret_cast<half4v*>(o + 32 * b + 2 * r + 4 * lh) = h;
+        }
+    } else {
+      float* rec = record(a, D, granule, head, kWide / 16, col);
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<float4v*>(rec + 32 * b + 2 * r + 4 * lh) =
+              float4v{acc[b][r], acc[b][r + 1], acc[b][r + 2], acc[b][r + 3]};
+      if (lh == 0) {
+        rec[D] = m;
+        rec[D + 1] = l;
+      }
+    }
+    return;
+  }
+  narrow_part<D>(a, s.n, a.q + at_row * D, limit, head, k);
   // The four wavefronts' sums, joined; thread: row, 4 dimensions.
   for (int e = threadIdx.x; e < 16 * (D / 4); e += 256) {
     const int r = e / (D / 4), d4 = e % (D / 4);
     if (row0 + r >= rows) continue;
-    const float mx = fmaxf(fmaxf(s.m[0][r], s.m[1][r]), fmaxf(s.m[2][r], s.m[3][r]));
+    const float mx = fmaxf(fmaxf(s.n.m[0][r], s.n.m[1][r]), fmaxf(s.n.m[2][r], s.n.m[3][r]));
     float4v o{0.0f, 0.0f, 0.0f, 0.0f};
     float l = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(s.m[w][r] - mx);
-      l = fmaf(s.l[w][r], f, l);
-      const float4v v = *reinterpret_cast<const float4v*>(&s.acc[w][r][4 * d4]);
+      const float f = __builtin_amdgcn_exp2f(s.n.m[w][r] - mx);
+      l = fmaf(s.n.l[w][r], f, l);
+      const float4v v = *reinterpret_cast<const float4v*>(&s.n.acc[w][r][4 * d4]);
 #pragma unroll
       for (int c = 0; c < 4; ++c) o[c] = fmaf(v[c], f, o[c]);
     }
@@ -432,7 +669,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnArgs a) {
       for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(none ? 0.0f : o[c] / l);
       *reinterpret_cast<half4v*>(a.out + (static_cast<int64_t>(tk) * hq + head * a.group + rr % a.group) * D + 4 * d4) = h;
     } else {
-      float* rec = record(a, D, granule, head, kTile / 16, r);
+      float* rec = record(a, D, granule, head, kNarrow / 16, r);
       *reinterpret_cast<float4v*>(rec + 4 * d4) = o;
       if (d4 == 0) {
         rec[D] = mx;
@@ -444,96 +681,108 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnArgs a) {
 
 // The parts of the rows of one token and KV head, joined: prefix parts first, then
 // the request's own, each with its weight relative to the largest maximum so far.
+// A workgroup takes `steps` tokens in turn, since each works out the units first.
 template <int D>
-__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, int steps) {
   __shared__ Requests req;
   load_requests(req, a);
-  const int token = static_cast<int>(blockIdx.x / a.hkv), head = static_cast<int>(blockIdx.x % a.hkv);
-  if (token >= req.off[a.n_req]) return;
+  const int head = static_cast<int>(blockIdx.x % a.hkv);
   const Units u = make_units(req, a);
-  const int i = __builtin_amdgcn_readfirstlane(request_of(req, a.n_req, token));
-  const int owner = i / u.per;
-  int base = __builtin_amdgcn_readlane(u.granules_before, owner);
-  for (int x = owner * u.per; x < i; ++x) {
-    const Share sh = share_of(req, a, x, u.c);
-    base += sh.tiles * sh.splits * sh.granules;
-  }
-  const Share sh = share_of(req, a, i, u.c);
-  if (sh.granules == 0) return;                             // written by its only part
   const int prefix_len = a.prefix_pages << a.page_log2;
-  const int j = token - req.off[i], t = max(req.off[i + 1] - req.off[i], 0);
-  if (j < 0 || j >= t) return;                              // (offsets that do not rise)
-  const bool none = req.kv[i] - t + j + 1 <= 0;
   const int64_t hq = static_cast<int64_t>(a.hkv) * a.group;
-  for (int e = threadIdx.x; e < a.group * (D / 4); e += 256) {
-    const int gq = e / (D / 4), d4 = e % (D / 4);
-    const int row = j * a.group + gq, tile = row / kTile;   // of the request
-    const int last = min((tile + 1) * kTile, t * a.group) - 1;
-    const int seen = req.kv[i] - t + last / a.group + 1 - prefix_len;
-    const int blocks = seen > 0 ? (seen + kBlockKeys - 1) / kBlockKeys : 1;
-    const int own = ceil_div(blocks, u.c), parts = u.prefix_splits + own;
-    const int prow = token * a.group + gq;                  // of the batch
-    auto rec = [&](int s) __attribute__((always_inline)) {
-      const bool pre = s < u.prefix_splits;
-      const int granule = pre ? prow / kTile * u.prefix_splits * (kTile / 16) + s * (kTile / 16)
-                              : base + (tile * sh.splits + s - u.prefix_splits) * sh.granules;
-      return record(a, D, min(granule, a.granules - kTile / 16), head, kTile / 16, (pre ? prow : row) % kTile);
-    };
-    float mx = -FLT_MAX, l = 0.0f;
-    float4v o{0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int BATCH = 8;
-    for (int s0 = 0; s0 < parts; s0 += BATCH) {
-      float4v v[BATCH];
-      float ms[BATCH], ls[BATCH];
-#pragma unroll
-      for (int b = 0; b < BATCH; ++b) {
-        const float* p = rec(min(s0 + b, parts - 1));
-        v[b] = *reinterpret_cast<const float4v*>(p + 4 * d4);
-        ms[b] = p[D];
-        ls[b] = p[D + 1];
-      }
-      float mn = mx;
-#pragma unroll
-      for (int b = 0; b < BATCH; ++b) mn = fmaxf(mn, ms[b]);
-      const float f0 = __builtin_amdgcn_exp2f(mx - mn);
-      mx = mn;
-      l *= f0;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) o[c] *= f0;
-#pragma unroll
-      for (int b = 0; b < BATCH; ++b) {
-        if (s0 + b >= parts) continue;
-        const float f = __builtin_amdgcn_exp2f(ms[b] - mx);
-        l = fmaf(ls[b], f, l);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] = fmaf(v[b][c], f, o[c]);
-      }
+  const int first = static_cast<int>(blockIdx.x / a.hkv) * steps;
+  const int end = min(first + steps, req.off[a.n_req]);
+  for (int token = first; token < end; ++token) {
+    const int i = __builtin_amdgcn_readfirstlane(request_of(req, a.n_req, token));
+    const Share sh = share_of(req, a, i, u.c);
+    const int j = token - req.off[i], t = max(req.off[i + 1] - req.off[i], 0);
+    if (sh.granules == 0 || j < 0 || j >= t) continue;      // written by its only part (or offsets that do not rise)
+    const int owner = i / u.per;
+    int base = __builtin_amdgcn_readlane(u.granules_before, owner);
+    for (int x = owner * u.per; x < i; ++x) {
+      const Share before = share_of(req, a, x, u.c);
+      base += before.tiles * before.splits * before.granules;
     }
-    half4v h;
+    const bool none = req.kv[i] - t + j + 1 <= 0;
+    const int per = tile_rows(sh.rows);
+    for (int e = threadIdx.x; e < a.group * (D / 4); e += 256) {
+      const int gq = e / (D / 4), d4 = e % (D / 4);
+      const int row = j * a.group + gq, tile = row / per;   // of the request
+      const int last = min((tile + 1) * per, sh.rows) - 1;
+      const int seen = req.kv[i] - t + last / a.group + 1 - prefix_len;
+      const int blocks = seen > 0 ? (seen + kBlockKeys - 1) / kBlockKeys : 1;
+      const int own = ceil_div(blocks, u.c), parts = u.prefix_splits + own;
+      const int prow = token * a.group + gq;                // of the batch
+      auto rec = [&](int s) __attribute__((always_inline)) {
+        const bool pre = s < u.prefix_splits;
+        const int g = pre ? u.prefix_tile / 16 : sh.granules;
+        const int granule = pre ? (s * u.prefix_tiles + prow / u.prefix_tile) * g
+                                : base + ((s - u.prefix_splits) * sh.tiles + tile) * g;
+        return record(a, D, min(granule, a.granules - g), head, g, pre ? prow % u.prefix_tile : row % per);
+      };
+      float mx = -FLT_MAX, l = 0.0f;
+      float4v o{0.0f, 0.0f, 0.0f, 0.0f};
+      constexpr int BATCH = 8;
+      for (int s0 = 0; s0 < parts; s0 += BATCH) {
+        float4v v[BATCH];
+        float ms[BATCH], ls[BATCH];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(none ? 0.0f : o[c] / l);
-    *reinterpret_cast<half4v*>(a.out + (static_cast<int64_t>(token) * hq + head * a.group + gq) * D + 4 * d4) = h;
+        for (int b = 0; b < BATCH; ++b) {
+          const float* p = rec(min(s0 + b, parts - 1));
+          v[b] = *reinterpret_cast<const float4v*>(p + 4 * d4);
+          ms[b] = p[D];
+          ls[b] = p[D + 1];
+        }
+        float mn = mx;
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) mn = fmaxf(mn, ms[b]);
+        const float f0 = __builtin_amdgcn_exp2f(mx - mn);
+        mx = mn;
+        l *= f0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] *= f0;
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+          if (s0 + b >= parts) continue;
+          const float f = __builtin_amdgcn_exp2f(ms[b] - mx);
+          l = fmaf(ls[b], f, l);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) o[c] = fmaf(v[b][c], f, o[c]);
+        }
+      }
+      half4v h;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(none ? 0.0f : o[c] / l);
+      *reinterpret_cast<half4v*>(a.out + (static_cast<int64_t>(token) * hq + head * a.group + gq) * D + 4 * d4) = h;
+    }
   }
 }
 
 // Workgroups per KV head that the keys are split for: about two per CU.
 int target_of(int hkv, int cu_count) { return std::max(1, (2 * cu_count + hkv - 1) / hkv); }
 
-// Tiles of the requests (and as many again of the prefix part at most): whole ones
-// and one begun per request with tokens.
-int64_t most_tiles(int64_t n_req, int64_t tokens, int64_t group) {
-  return tokens * group / kTile + std::min(n_req, tokens);
+// Most tiles of the requests: narrow ones, one per request with tokens at most, and
+// wide ones, whole ones and one begun per request of more than 16 rows.
+int64_t wide_tiles(int64_t n_req, int64_t tokens, int64_t group) {
+  return tokens * group / kWide + std::min(n_req, tokens * group / (kNarrow + 1));
 }
-int64_t prefix_tiles(int64_t tokens, int64_t group) { return (tokens * group + kTile - 1) / kTile; }
+int64_t most_tiles(int64_t n_req, int64_t tokens, int64_t group) {
+  return wide_tiles(n_req, tokens, group) + std::min(n_req, tokens);
+}
+int64_t prefix_tiles(int64_t tokens, int64_t group) { return (tokens * group + kWide - 1) / kWide; }
 
 }  // namespace
 
 size_t attn_paged_workspace_bytes(int32_t hq, int32_t hkv, int32_t d, int64_t n_req, int64_t tokens, bool prefix,
                                   int cu_count) {
   const int64_t target = target_of(hkv, cu_count), group = hq / hkv;
-  // Without a prefix only tiles of two or more splits leave parts: ceil(b / c) <= 2 b / c there.
-  const int64_t units = prefix ? most_tiles(n_req, tokens, group) + prefix_tiles(tokens, group) + target : 2 * target;
-  return static_cast<size_t>(units * (kTile / 16)) * hkv * 16 * (d + 4) * sizeof(float);
+  // Splits of c blocks: sum tiles ceil(blocks / c) <= tiles + target, and 2 target
+  // over the tiles with two or more, which alone leave parts where there is no prefix.
+  const int64_t granules =
+      prefix ? std::min(n_req, tokens) +
+                   (wide_tiles(n_req, tokens, group) + prefix_tiles(tokens, group) + target) * (kWide / 16)
+             : 2 * target * (kWide / 16);
+  return static_cast<size_t>(granules) * hkv * 16 * (d + 4) * sizeof(float);
 }
 
 hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, size_t ws_bytes, int cu_count, hipStream_t st) {
@@ -543,13 +792,15 @@ hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, size_t ws_bytes, int cu
       std::min<size_t>(ws_bytes / (static_cast<size_t>(a.hkv) * 16 * (d + 4) * sizeof(float)), INT32_MAX));
   const int64_t units = most_tiles(a.n_req, a.tokens, a.group) + a.target +
                         (a.prefix_pages ? prefix_tiles(a.tokens, a.group) : 0);
-  const dim3 grid(static_cast<unsigned>(units * a.hkv)), join(static_cast<unsigned>(static_cast<int64_t>(a.tokens) * a.hkv));
+  // About 2,048 workgroups join the parts.
+  const int steps = static_cast<int>((static_cast<int64_t>(a.tokens) * a.hkv + 2047) / 2048);
+  const dim3 grid(static_cast<unsigned>(units * a.hkv)), join(static_cast<unsigned>((a.tokens + steps - 1) / steps * a.hkv));
   if (d == 64) {
     hipLaunchKernelGGL(paged_attn_kernel<64>, grid, dim3(256), 0, st, a);
-    hipLaunchKernelGGL(paged_attn_join_kernel<64>, join, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(paged_attn_join_kernel<64>, join, dim3(256), 0, st, a, steps);
   } else {
     hipLaunchKernelGGL(paged_attn_kernel<128>, grid, dim3(256), 0, st, a);
-    hipLaunchKernelGGL(paged_attn_join_kernel<128>, join, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(paged_attn_join_kernel<128>, join, dim3(256), 0, st, a, steps);
   }
   return hipGetLastError();
 }

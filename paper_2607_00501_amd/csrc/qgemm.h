@@ -57,6 +57,7 @@
 #include <utility>
 
 #include "chunk.h"
+#include "lds_dma.h"
 #include "qm_internal.h"
 
 namespace qm {
@@ -106,53 +107,11 @@ __host__ __device__ constexpr int step_column(int step, int steps) {
 static_assert(step_column(3, 4) == 192 && step_column(6, 4) == 192 && step_column(0, 1) == 0);
 static_assert(step_column((1 << 25) + 2, 1 << 25) + 56 <= INT32_MAX - 7);
 
-// s_waitcnt vmcnt(N) with expcnt and lgkmcnt left free (gfx9 encoding:
-// vmcnt[3:0] in bits 3:0 and vmcnt[5:4] in bits 15:14).
-template <int N>
-__device__ __forceinline__ void vm_wait() {
-  static_assert(N >= 0 && N <= 63, "vmcnt is 6 bits");
-  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
-}
-
 // vm_wait<BASE + live * PER>() for a wavefront-uniform live in [0, L...]
 // (s_waitcnt takes an immediate: one scalar branch per candidate).
 template <int BASE, int PER, int... L>
 __device__ __forceinline__ void vm_wait_live(int live, std::integer_sequence<int, L...>) {
   ((live == L ? vm_wait<BASE + L * PER>() : void()), ...);
-}
-
-// 16 bytes per lane from global memory straight into LDS: lane l of the
-// wavefront writes lds_dst + 16 l (lds_dst is wavefront-uniform and goes
-// to M0).  Issued as inline asm so that the compiler's wait-count tracking
-// does not see it: with an LDS DMA pending, that tracking would wait for
-// every outstanding load (vmcnt 0) before the next use of any loaded
-// register.  The hardware still counts it in vmcnt; the kernel waits for it
-// explicitly (vm_wait), and every later wait the compiler computes stays
-// conservative.  The s_nop is the wait state gfx9 needs between a scalar write
-// of M0 and an LDS DMA, which the assembler does not add inside inline asm:
-// without it the DMA may take the previous M0 (1 KiB of a tile lands on the piece
-// before).
-__device__ __forceinline__ uint32_t lds_address(const void* p) {
-  return static_cast<uint32_t>(reinterpret_cast<size_t>((const void __attribute__((address_space(3)))*)p));
-}
-template <bool NT = false>
-__device__ __forceinline__ void lds_dma16(const void* src, const void* lds_dst) {
-  if constexpr (NT)
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(src), "s"(lds_address(lds_dst))
-                 : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds_address(lds_dst))
-                 : "memory", "m0");
-}
-// 4 bytes per lane, lane l to lds_dst + 4 l.
-template <bool NT = false>
-__device__ __forceinline__ void lds_dma4(const void* src, const void* lds_dst) {
-  if constexpr (NT)
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off nt" : : "v"(src), "s"(lds_address(lds_dst))
-                 : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(lds_address(lds_dst))
-                 : "memory", "m0");
 }
 
 // Dequantisation constants held in registers: the masks 0x000F000F and
