@@ -874,8 +874,11 @@ qm_status qkv_rope_append(const float* q, const float* k, const float* v, int32_
 // Heads and sizes of a paged attention call.
 static qm_status check_paged_heads(const char* name, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
   if (head_dim != 64 && head_dim != 128) return fail(QM_ESHAPE, "%s: head_dim=%d must be 64 or 128", name, head_dim);
-  if (n_kv_heads < 1 || n_kv_heads > 128 || n_q_heads < 1 || n_q_heads > 1024 || n_q_heads % n_kv_heads)
-    return fail(QM_ESHAPE, "%s: need n_kv_heads in [1, 128], n_q_heads in [1, 1024], a multiple of n_kv_heads", name);
+  if (n_kv_heads < 1 || n_kv_heads > 128 || n_q_heads < 1 || n_q_heads > 1024 || n_q_heads % n_kv_heads ||
+      n_q_heads / n_kv_heads > 128)
+    return fail(QM_ESHAPE,
+                "%s: need n_kv_heads in [1, 128], n_q_heads in [1, 1024], a multiple of n_kv_heads of at most 128 times",
+                name);
   return QM_OK;
 }
 
@@ -888,7 +891,7 @@ qm_status qattn_paged_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int
   if ((st = check_batch(name, n_req, kKvMaxTablePages, prefix_pages, tokens)) != QM_OK) return st;
   const DeviceInfo* d;
   if ((st = device_info(&d)) != QM_OK) return st;
-  *bytes = attn_paged_workspace_bytes(n_q_heads, n_kv_heads, head_dim, n_req, tokens, prefix_pages > 0, d->cu_count);
+  *bytes = attn_paged_workspace_bytes(n_q_heads, n_kv_heads, head_dim, tokens, prefix_pages > 0, d->cu_count);
   return QM_OK;
 }
 
@@ -914,7 +917,7 @@ qm_status qattn_paged_f16(const uint16_t* q, const uint16_t* k_pages, const uint
   const DeviceInfo* d;
   if ((st = device_info(&d)) != QM_OK) return st;
   const size_t need =
-      attn_paged_workspace_bytes(n_q_heads, n_kv_heads, head_dim, n_req, tokens, prefix_pages > 0, d->cu_count);
+      attn_paged_workspace_bytes(n_q_heads, n_kv_heads, head_dim, tokens, prefix_pages > 0, d->cu_count);
   if (!workspace || ws_bytes < need)
     return fail(QM_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", name, need, workspace ? ws_bytes : 0);
   a.q = q; a.k_pages = k_pages; a.v_pages = v_pages; a.tables = tables; a.prefix = prefix;
@@ -924,7 +927,7 @@ qm_status qattn_paged_f16(const uint16_t* q, const uint16_t* k_pages, const uint
   a.hkv = n_kv_heads; a.group = n_q_heads / n_kv_heads;
   a.max_pages = static_cast<int>(max_pages); a.n_pages = static_cast<int>(n_pages);
   a.prefix_pages = static_cast<int>(prefix_pages);
-  return launched(launch_attn_paged(a, head_dim, ws_bytes, d->cu_count, static_cast<hipStream_t>(stream)), name);
+  return launched(launch_attn_paged(a, head_dim, d->cu_count, static_cast<hipStream_t>(stream)), name);
 }
 
 qm_status qmoe_workspace_bytes(int64_t m, int32_t n_experts, int32_t top_k, int64_t hidden, int64_t inter,

@@ -14,18 +14,23 @@
 // are joined by a second launch, in a fixed order.
 //
 // The rows of one KV head are the batch's (token, query head of the group)
-// pairs, token-major.  Work units, one workgroup each per KV head:
-//   prefix part:  a tile of rows of any requests  x  a range of prefix keys,
-//   own part:     a tile of one request's rows    x  a range of its own keys.
-// Which units there are follows from the offsets and lengths on the device;
-// every workgroup works it out by itself with two sums over the requests, so
-// the call needs no host copy of the lengths, no plan made before it, and can be
-// replayed from a graph while the lengths move on.
+// pairs, token-major.  An item is a tile of rows with all the keys that it needs:
+//   prefix items:  a tile of rows of any requests  x  the prefix keys,
+//   own items:     a tile of one request's rows    x  its own keys.
+// The items of a KV head, laid end to end and each as long as it costs, are cut
+// into equal lengths, one for each workgroup that the CUs hold at once: every
+// workgroup has the same to do whatever the lengths of the requests, and at most
+// its first and its last item are parts that have to be joined.  Which items there
+// are follows from the offsets and lengths on the device; every workgroup works it
+// out by itself with two sums over the requests, so the call needs no host copy of
+// the lengths, no plan made before it, and can be replayed from a graph while the
+// lengths move on.
 #include "lds_dma.h"
 #include "qm_internal.h"
 
 #include <algorithm>
 #include <cfloat>
+#include <cstdio>
 
 namespace qm {
 namespace {
@@ -33,8 +38,7 @@ namespace {
 typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
-constexpr int kBlockKeys = 64;      // keys are split in multiples of this
-constexpr int kMinBlocks = 2;       // fewest blocks of a split
+constexpr int kBlockKeys = 64;      // keys are cut in multiples of this
 // Rows of a tile: 16 where a request (or the whole batch, for the prefix) has no
 // more, else 128.  The four wavefronts of a workgroup share the rows of the first
 // and split its keys, and split the rows of the second and share its keys.
@@ -74,90 +78,162 @@ __device__ __forceinline__ int request_of(const Requests& r, int n, int token) {
   return lo;
 }
 
-struct Share {
-  int rows, tiles, blocks, splits;
-  int granules;   // of 16 rows, that a tile leaves in the workspace; 0: its only part writes the output itself
+__device__ __forceinline__ int blocks_of(int keys) { return max((keys + kBlockKeys - 1) / kBlockKeys, 1); }
+
+// Inclusive sum over the lanes of a wavefront.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // row_shr:1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast:15, 31
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+// The same for 0 <= v < 2^49, in two halves.
+__device__ __forceinline__ int64_t wave_scan(int64_t v) {
+  const int lo = wave_scan(static_cast<int>(v & 0xFFFFFF)), hi = wave_scan(static_cast<int>(v >> 24));
+  return (static_cast<int64_t>(hi) << 24) + lo;
+}
+__device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
+  const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), lane));
+  return (static_cast<int64_t>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane)) << 32) | lo;
+}
+
+// Costs of an item beside its keys and of a block of 64 keys, for the two kinds of
+// tile, in what a block of the narrow kind costs.
+struct Cost { int item, block; };
+__device__ __forceinline__ Cost cost_of(const PagedAttnArgs& a, int per) {
+  return per == kWide ? Cost{a.wide_item, a.wide_block} : Cost{a.narrow_item, 1};
+}
+
+// The items of one request.
+struct Items {
+  int rows, per, tiles;
+  int64_t base;   // cost of a tile without the keys that its own rows bring
+  int slope;      // those: cost of a tile's, times 256
+  // Cost of the first j tiles.  Later tiles of a prompt see more keys.
+  __device__ int64_t cost(int j) const { return j * base + ((static_cast<int64_t>(slope) * j * (j + 1)) >> 9); }
 };
 
-__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+__device__ __forceinline__ Items items_of(const Requests& r, const PagedAttnArgs& a, int i) {
+  Items t;
+  const int tokens = max(r.off[i + 1] - r.off[i], 0), own = r.kv[i] - (a.prefix_pages << a.page_log2);
+  t.rows = tokens * a.group;
+  t.per = tile_rows(t.rows);
+  t.tiles = (t.rows + t.per - 1) / t.per;
+  const bool wide = t.per == kWide;
+  const Cost c = cost_of(a, t.per);
+  t.base = c.item + static_cast<int64_t>(c.block) * (wide ? max(own - tokens, 0) / kBlockKeys : blocks_of(own));
+  t.slope = wide ? c.block * 256 * kWide / (kBlockKeys * a.group) : 0;
+  return t;
+}
 
-// c: blocks per split (0: not known yet).
-__device__ __forceinline__ Share share_of(const Requests& r, const PagedAttnArgs& a, int i, int c) {
-  const int own = r.kv[i] - (a.prefix_pages << a.page_log2);
-  Share s;
-  s.rows = max(r.off[i + 1] - r.off[i], 0) * a.group;
-  const int per = tile_rows(s.rows);
-  s.tiles = (s.rows + per - 1) / per;
-  s.blocks = own > 0 ? (own + kBlockKeys - 1) / kBlockKeys : 1;
-  s.splits = c ? ceil_div(s.blocks, c) : 1;
-  s.granules = s.splits > 1 || a.prefix_pages ? per / 16 : 0;
+// Where the items lie on the line.  Every lane of a wavefront has `per` consecutive
+// requests; before: the cost of everything ahead of them.
+struct Line {
+  int per, prefix_rows, prefix_tile, prefix_tiles, prefix_cost;
+  int64_t before, total, chunk;
+};
+
+__device__ __forceinline__ Line make_line(const Requests& r, const PagedAttnArgs& a) {
+  const int lane = threadIdx.x & 63;
+  Line n;
+  n.per = (a.n_req + 63) / 64;
+  n.prefix_rows = a.prefix_pages ? r.off[a.n_req] * a.group : 0;
+  n.prefix_tile = tile_rows(n.prefix_rows);
+  n.prefix_tiles = (n.prefix_rows + n.prefix_tile - 1) / n.prefix_tile;
+  const Cost c = cost_of(a, n.prefix_tile);
+  n.prefix_cost = c.item + c.block * blocks_of(a.prefix_pages << a.page_log2);
+  int64_t cost = 0;
+  for (int i = lane * n.per; i < min((lane + 1) * n.per, a.n_req); ++i) {
+    const Items t = items_of(r, a, i);
+    cost += t.cost(t.tiles);
+  }
+  const int64_t upto = wave_scan(cost), prefix = static_cast<int64_t>(n.prefix_tiles) * n.prefix_cost;
+  n.before = prefix + upto - cost;
+  n.total = prefix + lane_value(upto, 63);
+  n.chunk = max<int64_t>(static_cast<int64_t>(static_cast<double>(n.total) * a.per_workgroup) + 1, a.min_chunk);
+  return n;
+}
+
+// What the launches that join the parts have to know, at the start of the
+// workspace.  Without a prefix: the item that workgroup w has begun and the next
+// `parts` ones go on with.  With one, where every row has parts: for each token,
+// for each tile (at the token of its first row) and for each prefix tile the
+// workgroups w0 .. w0 + n - 1 that go on with it.
+struct CutItem { int row, rows, parts, blind; };   // rows of the batch; the first `blind` see no key
+struct TokenInfo { int j, t, kv, per; };           // token j of t new ones, kv keys, rows of its request's tiles
+struct TileParts { int w0, n; };
+struct Space {
+  CutItem* cut;
+  TokenInfo* tokens;
+  TileParts* tiles;
+  TileParts* prefix_tiles;
+  float* records;
+  int workgroups, hq;
+};
+// Their bytes ahead of the records, a multiple of 16.
+__host__ __device__ __forceinline__ int64_t prefix_tiles_most(int64_t tokens, int64_t group) {
+  return (tokens * group + kWide - 1) / kWide;
+}
+__host__ __device__ __forceinline__ int64_t header_bytes(int workgroups, int64_t tokens, int64_t group, bool prefix) {
+  return prefix ? (tokens * static_cast<int64_t>(sizeof(TokenInfo) + sizeof(TileParts)) +
+                   prefix_tiles_most(tokens, group) * static_cast<int64_t>(sizeof(TileParts)) + 15) / 16 * 16
+                : workgroups * static_cast<int64_t>(sizeof(CutItem));
+}
+
+// Records, (D + 4) floats a row (D sums, maximum, sum of weights, 2 unused):
+// 128 rows per workgroup and KV head for a part that goes on from the workgroup
+// before, then as many for one that the next goes on with; with a prefix, in place
+// of those, one per row for the first part of the own keys and one for the prefix.
+template <int D>
+__device__ __forceinline__ float* row_record(const Space& s, int64_t row) { return s.records + row * (D + 4); }
+template <int D>
+__device__ __forceinline__ float* going_on(const Space& s, const PagedAttnArgs& a, int w, int head, int row) {
+  return row_record<D>(s, (static_cast<int64_t>(w) * a.hkv + head) * kWide + row);
+}
+template <int D>
+__device__ __forceinline__ float* begun(const Space& s, const PagedAttnArgs& a, int w, int head, int row) {
+  return going_on<D>(s, a, s.workgroups + w, head, row);
+}
+// at: (token, query head) as an element of [tokens][heads].
+template <int D>
+__device__ __forceinline__ float* own_row(const Space& s, const PagedAttnArgs& a, int64_t at) {
+  return row_record<D>(s, static_cast<int64_t>(s.workgroups) * a.hkv * kWide + at);
+}
+template <int D>
+__device__ __forceinline__ float* prefix_row(const Space& s, const PagedAttnArgs& a, int64_t at) {
+  return own_row<D>(s, a, static_cast<int64_t>(a.tokens) * s.hq + at);
+}
+
+__device__ __forceinline__ Space space_of(const PagedAttnArgs& a) {
+  Space s;
+  s.cut = reinterpret_cast<CutItem*>(a.ws);
+  s.tokens = reinterpret_cast<TokenInfo*>(a.ws);
+  s.tiles = reinterpret_cast<TileParts*>(s.tokens + a.tokens);
+  s.prefix_tiles = s.tiles + a.tokens;
+  s.records = a.ws + header_bytes(a.workgroups, a.tokens, a.group, a.prefix_pages > 0) / 4;
+  s.workgroups = a.workgroups;
+  s.hq = a.hkv * a.group;
   return s;
 }
 
-// Every lane of a wavefront takes `per` consecutive requests; units_before and
-// granules_before are the sums over the earlier lanes' requests.
-struct Units {
-  int c, per, prefix_tile, prefix_tiles, prefix_splits, units_before, granules_before, total;
-};
-
-template <class T>
-__device__ __forceinline__ T wave_scan(T v) {   // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const T o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
-}
-
-__device__ __forceinline__ Units make_units(const Requests& r, const PagedAttnArgs& a) {
-  const int lane = threadIdx.x & 63;
-  Units u;
-  u.per = (a.n_req + 63) / 64;
-  const int lo = lane * u.per, hi = min(lo + u.per, a.n_req);
-  int64_t work = 0;
-  for (int i = lo; i < hi; ++i) {
-    const Share s = share_of(r, a, i, 0);
-    work += static_cast<int64_t>(s.tiles) * s.blocks;
-  }
-  work = __shfl(wave_scan(work), 63);
-  const int prefix_blocks = ((a.prefix_pages << a.page_log2) + kBlockKeys - 1) / kBlockKeys;
-  const int rows = r.off[a.n_req] * a.group;
-  u.prefix_tile = tile_rows(rows);
-  u.prefix_tiles = a.prefix_pages ? ceil_div(rows, u.prefix_tile) : 0;
-  work += static_cast<int64_t>(u.prefix_tiles) * prefix_blocks;
-  // Splits of c blocks: sum tiles ceil(blocks / c) <= tiles + target.
-  u.c = static_cast<int>(max<int64_t>(kMinBlocks, (work + a.target - 1) / a.target));
-  u.prefix_splits = a.prefix_pages ? ceil_div(prefix_blocks, u.c) : 0;
-  int units = 0, granules = 0;
-  for (int i = lo; i < hi; ++i) {
-    const Share s = share_of(r, a, i, u.c);
-    units += s.tiles * s.splits;
-    granules += s.tiles * s.splits * s.granules;
-  }
-  const int units_to = wave_scan(units), granules_to = wave_scan(granules);
-  const int p = u.prefix_tiles * u.prefix_splits;
-  u.units_before = p + units_to - units;
-  u.granules_before = p * (u.prefix_tile / 16) + granules_to - granules;
-  u.total = p + __shfl(units_to, 63);
-  return u;
-}
-
 // ---------------------------------------------------- one part of one tile
+
+// The thread's index as the compiler may not know it: what depends on it is worked
+// out again for every item instead of being kept in registers across both kinds.
+__device__ __forceinline__ int fresh_thread() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
 
 // A range of keys behind a page table.
 struct Keys {
   const int32_t* pages;   // page ids of positions 0, page, 2 page, ...
   int lo, hi;             // this part's keys: positions [lo, hi); lo is a multiple of 16
 };
-
-// Record of a row in a part: D sums, maximum, sum of weights, 2 pad floats.
-__device__ __forceinline__ float* record(const PagedAttnArgs& a, int d, int granule, int head, int granules_per_head,
-                                         int row) {
-  return a.ws + ((static_cast<int64_t>(granule) * a.hkv + static_cast<int64_t>(head) * granules_per_head) * 16 + row) *
-                    (d + 4);
-}
 
 // An fp16 fragment with its infinities and NaNs as 0; seen is set if there were any.
 __device__ __forceinline__ half8v finite_part(half8v v, bool& seen) {
@@ -227,8 +303,8 @@ template <int D>
 __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, NarrowLds<D>& s, const uint16_t* q_row, int limit,
                                             int head, const Keys& k) {
   constexpr int KS = D / 32, DB = D / 16, VL = D / 16;   // k steps of S, dimension tiles, V loads per lane
-  const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int thread = fresh_thread(), lane = thread & 63, col = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int page_rows = 1 << a.page_log2;
   int most = limit, least = limit > 0 ? limit : INT32_MAX;
 #pragma unroll
@@ -386,8 +462,8 @@ template <int D>
 __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s, const uint16_t* q_row, int limit,
                                           int head, const Keys& k, float16v (&acc)[D / 32], float& m, float& l) {
   constexpr int KS = D / 16, DB = D / 32, C = D / 8, PIECES = D / 32;   // PIECES: KiB of 16 keys
-  const int lane = threadIdx.x & 63, col = lane & 31, lh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int thread = fresh_thread(), lane = thread & 63, col = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int page_rows = 1 << a.page_log2, hi = k.hi;
   int most = limit, least = limit > 0 ? limit : INT32_MAX;
 #pragma unroll
@@ -400,7 +476,7 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
   half8v qf[KS];
 #pragma unroll
   for (int c = 0; c < KS; ++c) qf[c] = *reinterpret_cast<const half8v*>(q_row + 16 * c + 8 * lh);
-  if (threadIdx.x == 0) s.bad = 0;
+  if (thread == 0) s.bad = 0;
 #pragma unroll
   for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -546,263 +622,379 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
   if (s.bad) l = __builtin_nanf("");
 }
 
+// Workgroups that a CU holds at once, by registers and LDS.
 template <int D>
-__global__ __launch_bounds__(256, 2) void paged_attn_kernel(PagedAttnArgs a) {
+constexpr int kResident = D == 64 ? 3 : 2;
+
+template <int D>
+__global__ __launch_bounds__(256, kResident<D>) void paged_attn_kernel(PagedAttnArgs a) {
   __shared__ Requests req;
   __shared__ __attribute__((aligned(1024))) TileLds<D> s;
   load_requests(req, a);
-  const Units u = make_units(req, a);
-  const int head = static_cast<int>(blockIdx.x % a.hkv);
-  const int unit = static_cast<int>(blockIdx.x / a.hkv);
-  if (unit >= u.total) return;
-  const int prefix_len = a.prefix_pages << a.page_log2;
-  const int lane = threadIdx.x & 63;
-  int row0, rows, per, granule, i = 0;                      // tile: first row, counted over the batch or the request
-  Keys k;
-  bool direct = false;
-  const bool shared = unit < u.prefix_tiles * u.prefix_splits;
-  // Parts of the same keys follow each other: they share what the L2 holds.
-  if (shared) {
-    per = u.prefix_tile;
-    row0 = unit % u.prefix_tiles * per;
-    rows = req.off[a.n_req] * a.group;
-    const int part = unit / u.prefix_tiles;
-    granule = unit * (per / 16);
-    k = Keys{a.prefix, part * u.c * kBlockKeys, min(prefix_len, (part + 1) * u.c * kBlockKeys)};
-  } else {
-    // The lane whose requests hold the unit, then the request.
-    const uint64_t before = __builtin_amdgcn_ballot_w64(u.units_before <= unit);
-    const int owner = 63 - __builtin_clzll(before);
-    int at = __builtin_amdgcn_readlane(u.units_before, owner);
-    granule = __builtin_amdgcn_readlane(u.granules_before, owner);
-    i = owner * u.per;
-    const int end = min(i + u.per, a.n_req);
-    Share sh = share_of(req, a, i, u.c);
-    while (at + sh.tiles * sh.splits <= unit && i + 1 < end) {
-      at += sh.tiles * sh.splits;
-      granule += sh.tiles * sh.splits * sh.granules;
-      sh = share_of(req, a, ++i, u.c);
-    }
-    rows = sh.rows;
-    per = tile_rows(rows);
-    row0 = (unit - at) % sh.tiles * per;
-    const int part = (unit - at) / sh.tiles;
-    granule += (unit - at) * sh.granules;
-    direct = sh.granules == 0;
-    // Splits past the keys that the tile's last row sees have nothing to do
-    // (the first is always there, so that every row is written).
-    const int last = min(row0 + per, rows) - 1;
-    const int seen = req.kv[i] - rows / a.group + last / a.group + 1;
-    const int64_t lo = prefix_len + static_cast<int64_t>(part) * u.c * kBlockKeys;
-    if (part > 0 && lo >= seen) return;
-    k = Keys{a.tables + static_cast<int64_t>(i) * a.max_pages, static_cast<int>(lo),
-             static_cast<int>(min<int64_t>(min(req.kv[i], seen), lo + static_cast<int64_t>(u.c) * kBlockKeys))};
-  }
-  if (!direct && granule + per / 16 > a.granules) return;   // (the workspace covers every batch of these limits)
-  // This lane's row of the tile.
-  const bool narrow = per == kNarrow;
-  const int col = narrow ? lane & 15 : static_cast<int>(threadIdx.x >> 6) * 32 + (lane & 31);
-  const int row = min(row0 + col, rows - 1);
-  int token = row / a.group;
-  const int gq = row % a.group;
-  if (shared) i = request_of(req, a.n_req, token);
-  else token += req.off[i];
-  const int j = token - req.off[i], t = max(req.off[i + 1] - req.off[i], 0);
-  const int sees = max(min(req.kv[i] - t + j + 1, req.kv[i]), 0);
-  const int limit = row0 + col >= rows ? 0 : shared ? min(sees, prefix_len) : sees;
-  const int64_t hq = static_cast<int64_t>(a.hkv) * a.group;
-  const int64_t at_row = static_cast<int64_t>(token) * hq + head * a.group + gq;   // of q and out
-  if (!narrow) {
-    float16v acc[D / 32];
-    float m, l;
-    wide_part<D>(a, s.w, a.q + at_row * D, limit, head, k, acc, m, l);
-    if (row0 + col >= rows) return;
-    const int lh = lane >> 5;
-    if (direct) {
-      const float inv = sees ? 1.0f / l : 0.0f;
-      uint16_t* o = a.out + at_row * D;
-#pragma unroll
-      for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          half4v h;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(sees ? acc[b][r + c] * inv : 0.0f);
-          *reinterpret_cast<half4v*>(o + 32 * b + 2 * r + 4 * lh) = h;
-        }
-    } else {
-      float* rec = record(a, D, granule, head, kWide / 16, col);
-#pragma unroll
-      for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<float4v*>(rec + 32 * b + 2 * r + 4 * lh) =
-              float4v{acc[b][r], acc[b][r + 1], acc[b][r + 2], acc[b][r + 3]};
-      if (lh == 0) {
-        rec[D] = m;
-        rec[D + 1] = l;
-      }
-    }
+  const Line line = make_line(req, a);
+  const Space space = space_of(a);
+  const int head = static_cast<int>(blockIdx.x % a.hkv), wg = static_cast<int>(blockIdx.x / a.hkv);
+  const int64_t x0 = wg * line.chunk, x1 = min(x0 + line.chunk, line.total);   // this workgroup's length of the line
+  bool begins = false;                                      // an item that the next workgroup goes on with
+  if (x0 >= line.total) {
+    if (!a.prefix_pages && head == 0 && threadIdx.x == 0) space.cut[wg].parts = 0;
     return;
   }
-  narrow_part<D>(a, s.n, a.q + at_row * D, limit, head, k);
-  // The four wavefronts' sums, joined; thread: row, 4 dimensions.
-  for (int e = threadIdx.x; e < 16 * (D / 4); e += 256) {
-    const int r = e / (D / 4), d4 = e % (D / 4);
-    if (row0 + r >= rows) continue;
-    const float mx = fmaxf(fmaxf(s.n.m[0][r], s.n.m[1][r]), fmaxf(s.n.m[2][r], s.n.m[3][r]));
-    float4v o{0.0f, 0.0f, 0.0f, 0.0f};
-    float l = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(s.n.m[w][r] - mx);
-      l = fmaf(s.n.l[w][r], f, l);
-      const float4v v = *reinterpret_cast<const float4v*>(&s.n.acc[w][r][4 * d4]);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) o[c] = fmaf(v[c], f, o[c]);
-    }
-    if (direct) {
-      const int rr = row0 + r, tk = req.off[i] + rr / a.group;
-      const bool none = req.kv[i] - t + rr / a.group + 1 <= 0;
-      half4v h;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(none ? 0.0f : o[c] / l);
-      *reinterpret_cast<half4v*>(a.out + (static_cast<int64_t>(tk) * hq + head * a.group + rr % a.group) * D + 4 * d4) = h;
-    } else {
-      float* rec = record(a, D, granule, head, kNarrow / 16, r);
-      *reinterpret_cast<float4v*>(rec + 4 * d4) = o;
-      if (d4 == 0) {
-        rec[D] = mx;
-        rec[D + 1] = l;
-      }
-    }
-  }
-}
-
-// The parts of the rows of one token and KV head, joined: prefix parts first, then
-// the request's own, each with its weight relative to the largest maximum so far.
-// A workgroup takes `steps` tokens in turn, since each works out the units first.
-template <int D>
-__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a, int steps) {
-  __shared__ Requests req;
-  load_requests(req, a);
-  const int head = static_cast<int>(blockIdx.x % a.hkv);
-  const Units u = make_units(req, a);
   const int prefix_len = a.prefix_pages << a.page_log2;
-  const int64_t hq = static_cast<int64_t>(a.hkv) * a.group;
-  const int first = static_cast<int>(blockIdx.x / a.hkv) * steps;
-  const int end = min(first + steps, req.off[a.n_req]);
-  for (int token = first; token < end; ++token) {
-    const int i = __builtin_amdgcn_readfirstlane(request_of(req, a.n_req, token));
-    const Share sh = share_of(req, a, i, u.c);
-    const int j = token - req.off[i], t = max(req.off[i + 1] - req.off[i], 0);
-    if (sh.granules == 0 || j < 0 || j >= t) continue;      // written by its only part (or offsets that do not rise)
-    const int owner = i / u.per;
-    int base = __builtin_amdgcn_readlane(u.granules_before, owner);
-    for (int x = owner * u.per; x < i; ++x) {
-      const Share before = share_of(req, a, x, u.c);
-      base += before.tiles * before.splits * before.granules;
+  const int64_t hq = space.hq;
+  // The item at x0: a prefix tile, or a request and a tile of it; it starts at `start`.
+  const int64_t prefix_end = static_cast<int64_t>(line.prefix_tiles) * line.prefix_cost;
+  int i = -1, tile = 0;                                     // request (-1: the prefix), tile
+  int64_t start = 0, req_start = prefix_end;
+  Items it{line.prefix_rows, line.prefix_tile, line.prefix_tiles, line.prefix_cost, 0};
+  if (x0 < prefix_end) {
+    tile = static_cast<int>(static_cast<double>(x0) / line.prefix_cost);
+    tile -= it.cost(tile) > x0;
+    tile += it.cost(tile + 1) <= x0;
+    start = it.cost(tile);
+  } else {
+    const uint64_t at = __builtin_amdgcn_ballot_w64(line.before <= x0);
+    const int owner = 63 - __builtin_clzll(at);
+    req_start = lane_value(line.before, owner);
+    i = owner * line.per;
+    it = items_of(req, a, i);
+    while (req_start + it.cost(it.tiles) <= x0 && i + 1 < a.n_req) {
+      req_start += it.cost(it.tiles);
+      it = items_of(req, a, ++i);
     }
-    const bool none = req.kv[i] - t + j + 1 <= 0;
-    const int per = tile_rows(sh.rows);
-    for (int e = threadIdx.x; e < a.group * (D / 4); e += 256) {
-      const int gq = e / (D / 4), d4 = e % (D / 4);
-      const int row = j * a.group + gq, tile = row / per;   // of the request
-      const int last = min((tile + 1) * per, sh.rows) - 1;
-      const int seen = req.kv[i] - t + last / a.group + 1 - prefix_len;
-      const int blocks = seen > 0 ? (seen + kBlockKeys - 1) / kBlockKeys : 1;
-      const int own = ceil_div(blocks, u.c), parts = u.prefix_splits + own;
-      const int prow = token * a.group + gq;                // of the batch
-      auto rec = [&](int s) __attribute__((always_inline)) {
-        const bool pre = s < u.prefix_splits;
-        const int g = pre ? u.prefix_tile / 16 : sh.granules;
-        const int granule = pre ? (s * u.prefix_tiles + prow / u.prefix_tile) * g
-                                : base + ((s - u.prefix_splits) * sh.tiles + tile) * g;
-        return record(a, D, min(granule, a.granules - g), head, g, pre ? prow % u.prefix_tile : row % per);
-      };
-      float mx = -FLT_MAX, l = 0.0f;
-      float4v o{0.0f, 0.0f, 0.0f, 0.0f};
-      constexpr int BATCH = 8;
-      for (int s0 = 0; s0 < parts; s0 += BATCH) {
-        float4v v[BATCH];
-        float ms[BATCH], ls[BATCH];
-#pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-          const float* p = rec(min(s0 + b, parts - 1));
-          v[b] = *reinterpret_cast<const float4v*>(p + 4 * d4);
-          ms[b] = p[D];
-          ls[b] = p[D + 1];
-        }
-        float mn = mx;
-#pragma unroll
-        for (int b = 0; b < BATCH; ++b) mn = fmaxf(mn, ms[b]);
-        const float f0 = __builtin_amdgcn_exp2f(mx - mn);
-        mx = mn;
-        l *= f0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] *= f0;
-#pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-          if (s0 + b >= parts) continue;
-          const float f = __builtin_amdgcn_exp2f(ms[b] - mx);
-          l = fmaf(ls[b], f, l);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) o[c] = fmaf(v[b][c], f, o[c]);
+    int hi = it.tiles - 1;
+    while (tile < hi) {
+      const int mid = (tile + hi + 1) >> 1;
+      if (req_start + it.cost(mid) <= x0) tile = mid; else hi = mid - 1;
+    }
+    start = req_start + it.cost(tile);
+  }
+  for (;;) {
+    const bool shared = i < 0;
+    const int64_t end = (shared ? 0 : req_start) + it.cost(tile + 1);
+    const int row0 = tile * it.per, rows = it.rows, per = it.per;
+    const int last = min(row0 + per, rows) - 1, t = shared ? 0 : rows / a.group;
+    const int seen = shared ? prefix_len : min(req.kv[i], req.kv[i] - t + last / a.group + 1);   // keys of the last row
+    const int first_key = shared ? 0 : prefix_len;
+    const int blocks = blocks_of(seen - first_key);
+    // Blocks of the item ahead of a place on the line; what would be a very short
+    // part goes to its neighbour.
+    const Cost cost = cost_of(a, per);
+    const int min_part = per == kWide ? a.wide_part : a.narrow_part;
+    auto ahead = [&](int64_t x) __attribute__((always_inline)) {
+      const int64_t keys = max<int64_t>(min<int64_t>(x - start - cost.item, INT32_MAX), -1);
+      const int b = static_cast<int>(keys) / cost.block;
+      return x >= end ? blocks : keys < 0 ? 0 : b > blocks - min_part ? blocks : b < min_part ? 0 : b;
+    };
+    const int from = ahead(x0), to = ahead(x1);
+    if (from < to) {
+      const int thread = fresh_thread(), lane = thread & 63;
+      if (from == 0 && head == 0) {
+        // Workgroups wg + 1 .. wg + n go on with the item: those whose length begins
+        // at the block blocks - min_part or before.
+        const int64_t left =
+            min(start + cost.item + static_cast<int64_t>(blocks - min_part + 1) * cost.block, end) - 1 - (wg + 1) * line.chunk;
+        const int n = to == blocks ? 0 : static_cast<int>(left / line.chunk) + 1;
+        if (!a.prefix_pages) {
+          // The rows of the batch, those of them that see no key.
+          if (n && thread == 0)
+            space.cut[wg] = CutItem{req.off[i] * a.group + row0, last + 1 - row0, n,
+                                    min(max((t - req.kv[i]) * a.group - row0, 0), kWide)};
+          begins = begins || n;
+        } else if (shared) {
+          if (thread == 0) space.prefix_tiles[tile] = TileParts{wg + 1, n};
+        } else {
+          if (thread == 0) space.tiles[req.off[i] + row0 / a.group] = TileParts{wg + 1, n};
+          // The tokens whose first row is in this tile.
+          for (int j = (row0 + a.group - 1) / a.group + thread; j * a.group <= last; j += 256)
+            space.tokens[req.off[i] + j] = TokenInfo{j, t, req.kv[i], per};
         }
       }
-      half4v h;
+      const bool whole = !a.prefix_pages && from == 0 && to == blocks;
+      Keys k;
+      k.pages = shared ? a.prefix : a.tables + static_cast<int64_t>(i) * a.max_pages;
+      k.lo = first_key + from * kBlockKeys;
+      k.hi = min(seen, first_key + to * kBlockKeys);
+      // This lane's row of the tile.
+      const bool narrow = per == kNarrow;
+      const int col = narrow ? lane & 15 : (thread >> 6) * 32 + (lane & 31);
+      const int row = min(row0 + col, last);
+      int token = row / a.group;
+      const int gq = row % a.group;
+      const int r = shared ? request_of(req, a.n_req, token) : i;
+      if (!shared) token += req.off[i];
+      const int sees = max(min(req.kv[r], req.kv[r] - max(req.off[r + 1] - token, 0) + 1), 0);
+      const int limit = row0 + col > last ? 0 : shared ? min(sees, prefix_len) : sees;
+      const int64_t at = token * hq + head * a.group + gq;  // of q and out
+      if (!narrow) {
+        float16v acc[D / 32];
+        float m, l;
+        wide_part<D>(a, s.w, a.q + at * D, limit, head, k, acc, m, l);
+        const int lh = lane >> 5;
+        if (row0 + col <= last) {
+          if (whole) {
+            const float inv = sees ? 1.0f / l : 0.0f;
+            uint16_t* o = a.out + at * D;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(none ? 0.0f : o[c] / l);
-      *reinterpret_cast<half4v*>(a.out + (static_cast<int64_t>(token) * hq + head * a.group + gq) * D + 4 * d4) = h;
+            for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+              for (int q = 0; q < 16; q += 4) {
+                half4v h;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(sees ? acc[b][q + c] * inv : 0.0f);
+                *reinterpret_cast<half4v*>(o + 32 * b + 2 * q + 4 * lh) = h;
+              }
+          } else {
+            float* rec = from ? going_on<D>(space, a, wg, head, col)
+                         : !a.prefix_pages ? begun<D>(space, a, wg, head, col)
+                         : shared ? prefix_row<D>(space, a, at) : own_row<D>(space, a, at);
+#pragma unroll
+            for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+              for (int q = 0; q < 16; q += 4)
+                *reinterpret_cast<float4v*>(rec + 32 * b + 2 * q + 4 * lh) =
+                    float4v{acc[b][q], acc[b][q + 1], acc[b][q + 2], acc[b][q + 3]};
+            if (lh == 0) {
+              rec[D] = m;
+              rec[D + 1] = l;
+            }
+          }
+        }
+      } else {
+        narrow_part<D>(a, s.n, a.q + at * D, limit, head, k);
+        // The four wavefronts' sums, joined; thread: row, 4 dimensions.
+        for (int e = thread; e < 16 * (D / 4); e += 256) {
+          const int x = e / (D / 4), d4 = e % (D / 4);
+          if (row0 + x > last) continue;
+          const float mx = fmaxf(fmaxf(s.n.m[0][x], s.n.m[1][x]), fmaxf(s.n.m[2][x], s.n.m[3][x]));
+          float4v o{0.0f, 0.0f, 0.0f, 0.0f};
+          float l = 0.0f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(s.n.m[w][x] - mx);
+            l = fmaf(s.n.l[w][x], f, l);
+            const float4v v = *reinterpret_cast<const float4v*>(&s.n.acc[w][x][4 * d4]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[c] = fmaf(v[c], f, o[c]);
+          }
+          const int tk = (row0 + x) / a.group;              // of the request or the batch
+          const int64_t xat = ((shared ? 0 : req.off[i]) + tk) * hq + head * a.group + (row0 + x) % a.group;
+          if (whole) {
+            const bool none = req.kv[i] - t + tk + 1 <= 0;
+            half4v h;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(none ? 0.0f : o[c] / l);
+            *reinterpret_cast<half4v*>(a.out + xat * D + 4 * d4) = h;
+          } else {
+            float* rec = from ? going_on<D>(space, a, wg, head, x)
+                         : !a.prefix_pages ? begun<D>(space, a, wg, head, x)
+                         : shared ? prefix_row<D>(space, a, xat) : own_row<D>(space, a, xat);
+            *reinterpret_cast<float4v*>(rec + 4 * d4) = o;
+            if (d4 == 0) {
+              rec[D] = mx;
+              rec[D + 1] = l;
+            }
+          }
+        }
+      }
+      __syncthreads();                                      // the tile's LDS is free
     }
+    if (end >= x1) break;
+    start = end;
+    if (++tile == it.tiles) {
+      req_start = end;
+      tile = 0;
+      do {                                                  // (there is one: end < x1 <= total)
+        it = items_of(req, a, ++i);
+      } while (it.tiles == 0 && i + 1 < a.n_req);
+    }
+  }
+  if (!a.prefix_pages && !begins && head == 0 && threadIdx.x == 0) space.cut[wg].parts = 0;
+}
+
+// Parts s0, s0 + step, ... of a row, each with its weight relative to the largest
+// maximum so far; rec(s): the record of part s, d4: this thread's four dimensions.
+struct Joined { float4v o; float m, l; };
+template <int D, class Rec>
+__device__ __forceinline__ Joined join_parts(int s0, int step, int parts, int d4, Rec rec) {
+  constexpr int BATCH = 8;                                  // loads in flight
+  Joined r{float4v{0.0f, 0.0f, 0.0f, 0.0f}, -FLT_MAX, 0.0f};
+  for (; s0 < parts; s0 += BATCH * step) {
+    float4v v[BATCH];
+    float ms[BATCH], ls[BATCH];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const float* p = rec(min(s0 + b * step, parts - 1));
+      v[b] = *reinterpret_cast<const float4v*>(p + 4 * d4);
+      ms[b] = p[D];
+      ls[b] = p[D + 1];
+    }
+    float mn = r.m;
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) mn = fmaxf(mn, ms[b]);
+    const float f0 = __builtin_amdgcn_exp2f(r.m - mn);
+    r.m = mn;
+    r.l *= f0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) r.o[c] *= f0;
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (s0 + b * step >= parts) continue;
+      const float f = __builtin_amdgcn_exp2f(ms[b] - mn);
+      r.l = fmaf(ls[b], f, r.l);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) r.o[c] = fmaf(v[b][c], f, r.o[c]);
+    }
+  }
+  return r;
+}
+
+// The groups of `width` threads of a workgroup joined in order; whole workgroup.
+__device__ __forceinline__ Joined join_groups(Joined r, int groups, int width) {
+  __shared__ float4v part[256];
+  __shared__ float2 stat[256];
+  const int th = threadIdx.x % width;
+  part[threadIdx.x] = r.o;
+  stat[threadIdx.x] = make_float2(r.m, r.l);
+  __syncthreads();
+  r = Joined{float4v{0.0f, 0.0f, 0.0f, 0.0f}, -FLT_MAX, 0.0f};
+  for (int x = 0; x < groups; ++x) r.m = fmaxf(r.m, stat[x * width + th].x);
+  for (int x = 0; x < groups; ++x) {
+    const float2 st = stat[x * width + th];
+    const float f = __builtin_amdgcn_exp2f(st.x - r.m);
+    r.l = fmaf(st.y, f, r.l);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) r.o[c] = fmaf(part[x * width + th][c], f, r.o[c]);
+  }
+  return r;
+}
+
+template <int D>
+__device__ __forceinline__ void write_joined(const PagedAttnArgs& a, int64_t at, int d4, const Joined& r, bool none) {
+  half4v h;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(none ? 0.0f : r.o[c] / r.l);
+  *reinterpret_cast<half4v*>(a.out + at * D + 4 * d4) = h;
+}
+
+// Element of [tokens][heads] of a row of the batch.
+__device__ __forceinline__ int64_t element_of(const PagedAttnArgs& a, int row, int head) {
+  const int token = row / a.group;
+  return static_cast<int64_t>(token) * a.hkv * a.group + head * a.group + (row - token * a.group);
+}
+
+// Without a prefix: the items that are cut, a workgroup for 16 rows of each.  A row
+// has D / 4 threads, four dimensions each; with few rows several groups of threads
+// share its parts.
+template <int D>
+__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
+  constexpr int C4 = D / 4;
+  const Space space = space_of(a);
+  const int head = static_cast<int>(blockIdx.x % a.hkv), rest = static_cast<int>(blockIdx.x / a.hkv);
+  const int w = rest % a.workgroups, row0 = rest / a.workgroups * 16;
+  const CutItem it = space.cut[w];
+  const int rows = min(it.rows - row0, 16);
+  if (it.parts == 0 || rows <= 0) return;
+  int groups = 1;
+  while (2 * groups * rows * C4 <= 256 && 2 * groups <= it.parts) groups *= 2;
+  const int width = 256 / groups, grp = threadIdx.x / width;
+  for (int e = threadIdx.x % width; e < rows * C4 || groups > 1; e += width) {   // (once where there are several groups)
+    const int row = row0 + min(e / C4, rows - 1), d4 = e % C4;
+    auto rec = [&](int x) __attribute__((always_inline)) {
+      return x == 0 ? begun<D>(space, a, w, head, row) : going_on<D>(space, a, min(w + x, a.workgroups - 1), head, row);
+    };
+    Joined r = join_parts<D>(grp, groups, it.parts + 1, d4, rec);
+    if (groups > 1) r = join_groups(r, groups, width);
+    if (grp == 0 && e < rows * C4) write_joined<D>(a, element_of(a, it.row + row, head), d4, r, row < it.blind);
+    if (groups > 1) break;
   }
 }
 
-// Workgroups per KV head that the keys are split for: about two per CU.
-int target_of(int hkv, int cu_count) { return std::max(1, (2 * cu_count + hkv - 1) / hkv); }
+// With a prefix every row has parts: a workgroup of `groups` groups takes
+// 256 / groups / (D / 4) rows of the batch.
+template <int D>
+__global__ __launch_bounds__(256) void paged_attn_join_rows_kernel(PagedAttnArgs a, int groups) {
+  constexpr int C4 = D / 4;
+  const Space space = space_of(a);
+  const int head = static_cast<int>(blockIdx.x % a.hkv);
+  const int tokens = min(max(a.offsets[a.n_req], 0), a.tokens), rows = tokens * a.group;
+  const int width = 256 / groups, grp = threadIdx.x / width, th = threadIdx.x % width;
+  const int row = static_cast<int>(blockIdx.x / a.hkv) * (width / C4) + th / C4, d4 = th % C4;
+  if (row - th / C4 >= rows) return;                        // whole workgroup
+  const int token = min(row, rows - 1) / a.group, gq = min(row, rows - 1) - token * a.group;
+  const TokenInfo tp = space.tokens[token];
+  // (The test holds whatever lies there for a token of no request, where offsets do not rise.)
+  const bool there = row < rows && (tp.per == kNarrow || tp.per == kWide) && tp.j >= 0 && tp.j <= token;
+  const int per = there ? tp.per : kNarrow, own_row_at = there ? tp.j * a.group + gq : 0;   // row of the request
+  const int tile = own_row_at / per, prefix_tile = tile_rows(rows), prow = token * a.group + gq;
+  const TileParts own = space.tiles[there ? token - tp.j + tile * per / a.group : 0];
+  const TileParts pre = space.prefix_tiles[prow / prefix_tile];
+  const int64_t at = element_of(a, prow, head);
+  const int own_at = min(max(pre.n, 0), a.workgroups) + 1;  // parts of the prefix
+  const int parts = own_at + 1 + min(max(own.n, 0), a.workgroups);
+  auto rec = [&](int x) __attribute__((always_inline)) {
+    auto held = [&](int w) __attribute__((always_inline)) { return min(max(w, 0), a.workgroups - 1); };
+    if (x == 0) return prefix_row<D>(space, a, at);
+    if (x < own_at) return going_on<D>(space, a, held(pre.w0 + x - 1), head, prow % prefix_tile);
+    if (x == own_at) return own_row<D>(space, a, at);
+    return going_on<D>(space, a, held(own.w0 + x - own_at - 1), head, own_row_at % per);
+  };
+  Joined r = join_parts<D>(grp, groups, there ? parts : 0, d4, rec);
+  if (groups > 1) r = join_groups(r, groups, width);
+  if (grp == 0 && there) write_joined<D>(a, at, d4, r, tp.kv - tp.t + tp.j + 1 <= 0);
+}
 
-// Most tiles of the requests: narrow ones, one per request with tokens at most, and
-// wide ones, whole ones and one begun per request of more than 16 rows.
-int64_t wide_tiles(int64_t n_req, int64_t tokens, int64_t group) {
-  return tokens * group / kWide + std::min(n_req, tokens * group / (kNarrow + 1));
+// Workgroups per KV head: those that the CUs hold at once.
+int workgroups_of(int hkv, int d, int cu_count) {
+  return std::max(1, (d == 64 ? kResident<64> : kResident<128>) * cu_count / hkv);
 }
-int64_t most_tiles(int64_t n_req, int64_t tokens, int64_t group) {
-  return wide_tiles(n_req, tokens, group) + std::min(n_req, tokens);
-}
-int64_t prefix_tiles(int64_t tokens, int64_t group) { return (tokens * group + kWide - 1) / kWide; }
 
 }  // namespace
 
-size_t attn_paged_workspace_bytes(int32_t hq, int32_t hkv, int32_t d, int64_t n_req, int64_t tokens, bool prefix,
-                                  int cu_count) {
-  const int64_t target = target_of(hkv, cu_count), group = hq / hkv;
-  // Splits of c blocks: sum tiles ceil(blocks / c) <= tiles + target, and 2 target
-  // over the tiles with two or more, which alone leave parts where there is no prefix.
-  const int64_t granules =
-      prefix ? std::min(n_req, tokens) +
-                   (wide_tiles(n_req, tokens, group) + prefix_tiles(tokens, group) + target) * (kWide / 16)
-             : 2 * target * (kWide / 16);
-  return static_cast<size_t>(granules) * hkv * 16 * (d + 4) * sizeof(float);
+size_t attn_paged_workspace_bytes(int32_t hq, int32_t hkv, int32_t d, int64_t tokens, bool prefix, int cu_count) {
+  const int workgroups = workgroups_of(hkv, d, cu_count);
+  const int64_t slots = static_cast<int64_t>(workgroups) * hkv * kWide;
+  const int64_t records = prefix ? slots + 2 * tokens * hq : 2 * slots;
+  return static_cast<size_t>(header_bytes(workgroups, tokens, hq / hkv, prefix)) +
+         static_cast<size_t>(records) * (d + 4) * sizeof(float);
 }
 
-hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, size_t ws_bytes, int cu_count, hipStream_t st) {
-  if (a.tokens == 0) return hipSuccess;
-  a.target = target_of(a.hkv, cu_count);
-  a.granules = static_cast<int>(
-      std::min<size_t>(ws_bytes / (static_cast<size_t>(a.hkv) * 16 * (d + 4) * sizeof(float)), INT32_MAX));
-  const int64_t units = most_tiles(a.n_req, a.tokens, a.group) + a.target +
-                        (a.prefix_pages ? prefix_tiles(a.tokens, a.group) : 0);
-  // About 2,048 workgroups join the parts.
-  const int steps = static_cast<int>((static_cast<int64_t>(a.tokens) * a.hkv + 2047) / 2048);
-  const dim3 grid(static_cast<unsigned>(units * a.hkv)), join(static_cast<unsigned>((a.tokens + steps - 1) / steps * a.hkv));
-  if (d == 64) {
-    hipLaunchKernelGGL(paged_attn_kernel<64>, grid, dim3(256), 0, st, a);
-    hipLaunchKernelGGL(paged_attn_join_kernel<64>, join, dim3(256), 0, st, a, steps);
-  } else {
-    hipLaunchKernelGGL(paged_attn_kernel<128>, grid, dim3(256), 0, st, a);
-    hipLaunchKernelGGL(paged_attn_join_kernel<128>, join, dim3(256), 0, st, a, steps);
+namespace {
+
+template <int D>
+hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(paged_attn_kernel<D>, dim3(static_cast<unsigned>(a.workgroups * a.hkv)), dim3(256), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (!a.prefix_pages) {
+    hipLaunchKernelGGL(paged_attn_join_kernel<D>, dim3(static_cast<unsigned>(a.workgroups * a.hkv * (kWide / 16))), dim3(256),
+                       0, st, a);
+    return hipGetLastError();
   }
+  // More groups a row while that leaves at most about 1,024 workgroups.
+  const int64_t rows = static_cast<int64_t>(a.tokens) * a.group;
+  int groups = 1;
+  auto blocks = [&](int g) { return (rows + 256 / g / (D / 4) - 1) / (256 / g / (D / 4)) * a.hkv; };
+  while (2 * groups * (D / 4) <= 256 && blocks(2 * groups) <= 1024) groups *= 2;
+  hipLaunchKernelGGL(paged_attn_join_rows_kernel<D>, dim3(static_cast<unsigned>(blocks(groups))), dim3(256), 0, st, a, groups);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, int cu_count, hipStream_t st) {
+  if (a.tokens == 0) return hipSuccess;
+  a.workgroups = workgroups_of(a.hkv, d, cu_count);
+  a.per_workgroup = 1.0 / a.workgroups;
+  a.narrow_item = 1;
+  a.wide_item = 4;
+  a.wide_block = 2;
+  a.min_chunk = 4;
+  a.narrow_part = 2;
+  a.wide_part = 4;
+  if (const char* e = tuning_override("QM_PAGED_PLAN"))
+    std::sscanf(e, "%d,%d,%d,%d,%d,%d", &a.narrow_item, &a.wide_item, &a.wide_block, &a.min_chunk, &a.narrow_part, &a.wide_part);
+  return d == 64 ? launch_paged<64>(a, st) : launch_paged<128>(a, st);
 }
 
 }  // namespace qm

@@ -253,12 +253,14 @@ struct PagedAttnArgs {
   float* ws;
   float scale_log2;
   int n_req, tokens, hkv, group, page_log2, max_pages, n_pages, prefix_pages;
-  int target;                                     // workgroups per KV head that the keys are split for
-  int granules;                                   // 16-row granules that the workspace holds
+  // Set by the launch: workgroups per KV head (and one over it); costs of an item
+  // beside its keys and of 64 keys for a 128-row tile, in what 64 keys of a 16-row
+  // tile cost; the least that a workgroup takes; the fewest 64-key blocks of a part.
+  double per_workgroup;
+  int workgroups, narrow_item, wide_item, wide_block, min_chunk, narrow_part, wide_part;
 };
-size_t attn_paged_workspace_bytes(int32_t hq, int32_t hkv, int32_t d, int64_t n_req, int64_t tokens, bool prefix,
-                                  int cu_count);
-hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, size_t ws_bytes, int cu_count, hipStream_t st);
+size_t attn_paged_workspace_bytes(int32_t hq, int32_t hkv, int32_t d, int64_t tokens, bool prefix, int cu_count);
+hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, int cu_count, hipStream_t st);
 
 struct MoeArgs {
   const uint8_t* gq; const uint16_t* gs;   // gate [E][inter][hidden], device layout
