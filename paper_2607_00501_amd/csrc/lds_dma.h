@@ -40,6 +40,11 @@ __device__ __forceinline__ void lds_dma16(const void* src, const void* lds_dst) 
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds_address(lds_dst))
                  : "memory", "m0");
 }
+// The same from a wavefront-uniform address and a byte offset per lane.
+__device__ __forceinline__ void lds_dma16(const void* src, uint32_t offset, const void* lds_dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(src),
+               "s"(lds_address(lds_dst)) : "memory", "m0");
+}
 // 4 bytes per lane, lane l to lds_dst + 4 l.
 template <bool NT = false>
 __device__ __forceinline__ void lds_dma4(const void* src, const void* lds_dst) {

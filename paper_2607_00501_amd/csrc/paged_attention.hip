@@ -17,14 +17,18 @@
 // pairs, token-major.  An item is a tile of rows with all the keys that it needs:
 //   prefix items:  a tile of rows of any requests  x  the prefix keys,
 //   own items:     a tile of one request's rows    x  its own keys.
-// The items of a KV head, laid end to end and each as long as it costs, are cut
-// into equal lengths, one for each workgroup that the CUs hold at once: every
-// workgroup has the same to do whatever the lengths of the requests, and at most
-// its first and its last item are parts that have to be joined.  Which items there
-// are follows from the offsets and lengths on the device; every workgroup works it
-// out by itself with two sums over the requests, so the call needs no host copy of
-// the lengths, no plan made before it, and can be replayed from a graph while the
-// lengths move on.
+// Items of more than 16 rows are the work of a workgroup (128 rows, 32 per
+// wavefront, keys shared through LDS), bound by the MFMA; the others, a single
+// token's group of heads, of a wavefront by itself, bound by HBM.  The items of
+// each kind and KV head, laid end to end and each as long as it costs, are cut into
+// equal lengths, one for each workgroup (or wavefront) that the CUs hold at once:
+// all have the same to do whatever the lengths of the requests, and at most the
+// first and the last item of each are parts that have to be joined.  Half of the
+// workgroups take their length of the wide items first and half that of the narrow
+// ones, so that MFMA and HBM are busy together.  Which items there are follows from
+// the offsets and lengths on the device; every workgroup works it out by itself with
+// sums over the requests, so the call needs no host copy of the lengths, no plan
+// made before it, and can be replayed from a graph while the lengths move on.
 #include "lds_dma.h"
 #include "qm_internal.h"
 
@@ -38,7 +42,6 @@ namespace {
 typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
-constexpr int kBlockKeys = 64;      // keys are cut in multiples of this
 // Rows of a tile: 16 where a request (or the whole batch, for the prefix) has no
 // more, else 128.  The four wavefronts of a workgroup share the rows of the first
 // and split its keys, and split the rows of the second and share its keys.
@@ -78,7 +81,6 @@ __device__ __forceinline__ int request_of(const Requests& r, int n, int token) {
   return lo;
 }
 
-__device__ __forceinline__ int blocks_of(int keys) { return max((keys + kBlockKeys - 1) / kBlockKeys, 1); }
 
 // Inclusive sum over the lanes of a wavefront.
 __device__ __forceinline__ int wave_scan(int v) {
@@ -100,79 +102,124 @@ __device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
   return (static_cast<int64_t>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane)) << 32) | lo;
 }
 
-// Costs of an item beside its keys and of a block of 64 keys, for the two kinds of
-// tile, in what a block of the narrow kind costs.
-struct Cost { int item, block; };
-__device__ __forceinline__ Cost cost_of(const PagedAttnArgs& a, int per) {
-  return per == kWide ? Cost{a.wide_item, a.wide_block} : Cost{a.narrow_item, 1};
-}
+// The two kinds of item: rows of a tile, keys of a block, cost of an item beside
+// its keys in blocks (fetching the page ids and the queries, writing the result),
+// the fewest blocks of a part.
+enum Kind { kNarrowItem = 0, kWideItem = 1 };
+template <Kind K> constexpr int kRows = K == kWideItem ? kWide : kNarrow;
+template <Kind K> constexpr int kKeys = K == kWideItem ? 64 : 32;
+template <Kind K> __device__ __forceinline__ int blocks_of(int keys) { return max((keys + kKeys<K> - 1) / kKeys<K>, 1); }
 
-// The items of one request.
+// The items of one kind of one request (or of the prefix).
 struct Items {
-  int rows, per, tiles;
+  int rows, tiles;
   int64_t base;   // cost of a tile without the keys that its own rows bring
-  int slope;      // those: cost of a tile's, times 256
+  int slope;      // those: blocks per tile, times 256
   // Cost of the first j tiles.  Later tiles of a prompt see more keys.
-  __device__ int64_t cost(int j) const { return j * base + ((static_cast<int64_t>(slope) * j * (j + 1)) >> 9); }
+  __device__ __forceinline__ int64_t cost(int j) const {
+    return j * base + ((static_cast<int64_t>(slope) * j * (j + 1)) >> 9);
+  }
 };
 
+template <Kind K>
 __device__ __forceinline__ Items items_of(const Requests& r, const PagedAttnArgs& a, int i) {
   Items t;
   const int tokens = max(r.off[i + 1] - r.off[i], 0), own = r.kv[i] - (a.prefix_pages << a.page_log2);
   t.rows = tokens * a.group;
-  t.per = tile_rows(t.rows);
-  t.tiles = (t.rows + t.per - 1) / t.per;
-  const bool wide = t.per == kWide;
-  const Cost c = cost_of(a, t.per);
-  t.base = c.item + static_cast<int64_t>(c.block) * (wide ? max(own - tokens, 0) / kBlockKeys : blocks_of(own));
-  t.slope = wide ? c.block * 256 * kWide / (kBlockKeys * a.group) : 0;
+  t.tiles = tile_rows(t.rows) == kRows<K> ? (t.rows + kRows<K> - 1) / kRows<K> : 0;
+  t.base = a.item_cost[K] + (K == kWideItem ? max(own - tokens, 0) / kKeys<K> : blocks_of<K>(own));
+  t.slope = K == kWideItem ? 256 * kWide / (kKeys<K> * a.group) : 0;
   return t;
 }
 
-// Where the items lie on the line.  Every lane of a wavefront has `per` consecutive
-// requests; before: the cost of everything ahead of them.
+template <Kind K>
+__device__ __forceinline__ Items prefix_items(const Requests& r, const PagedAttnArgs& a) {
+  Items t{a.prefix_pages ? r.off[a.n_req] * a.group : 0, 0, 0, 0};
+  t.tiles = tile_rows(t.rows) == kRows<K> ? (t.rows + kRows<K> - 1) / kRows<K> : 0;
+  t.base = a.item_cost[K] + blocks_of<K>(a.prefix_pages << a.page_log2);
+  return t;
+}
+
+// The line of one kind.  Every lane of a wavefront has `per` consecutive requests;
+// before: the cost of everything ahead of them; chunk: the length that a worker takes.
 struct Line {
-  int per, prefix_rows, prefix_tile, prefix_tiles, prefix_cost;
+  int per;
   int64_t before, total, chunk;
 };
 
+template <Kind K>
 __device__ __forceinline__ Line make_line(const Requests& r, const PagedAttnArgs& a) {
   const int lane = threadIdx.x & 63;
   Line n;
   n.per = (a.n_req + 63) / 64;
-  n.prefix_rows = a.prefix_pages ? r.off[a.n_req] * a.group : 0;
-  n.prefix_tile = tile_rows(n.prefix_rows);
-  n.prefix_tiles = (n.prefix_rows + n.prefix_tile - 1) / n.prefix_tile;
-  const Cost c = cost_of(a, n.prefix_tile);
-  n.prefix_cost = c.item + c.block * blocks_of(a.prefix_pages << a.page_log2);
+  const Items shared = prefix_items<K>(r, a);
+  const int64_t prefix = shared.cost(shared.tiles);
   int64_t cost = 0;
   for (int i = lane * n.per; i < min((lane + 1) * n.per, a.n_req); ++i) {
-    const Items t = items_of(r, a, i);
+    const Items t = items_of<K>(r, a, i);
     cost += t.cost(t.tiles);
   }
-  const int64_t upto = wave_scan(cost), prefix = static_cast<int64_t>(n.prefix_tiles) * n.prefix_cost;
+  const int64_t upto = wave_scan(cost);
   n.before = prefix + upto - cost;
   n.total = prefix + lane_value(upto, 63);
-  n.chunk = max<int64_t>(static_cast<int64_t>(static_cast<double>(n.total) * a.per_workgroup) + 1, a.min_chunk);
+  n.chunk = max<int64_t>(static_cast<int64_t>(static_cast<double>(n.total) * a.per_worker[K]) + 1, a.min_chunk[K]);
   return n;
 }
 
-// What the launches that join the parts have to know, at the start of the
-// workspace.  Without a prefix: the item that workgroup w has begun and the next
-// `parts` ones go on with.  With one, where every row has parts: for each token,
-// for each tile (at the token of its first row) and for each prefix tile the
-// workgroups w0 .. w0 + n - 1 that go on with it.
-struct CutItem { int row, rows, parts, blind; };   // rows of the batch; the first `blind` see no key
-struct TokenInfo { int j, t, kv, per; };           // token j of t new ones, kv keys, rows of its request's tiles
-struct TileParts { int w0, n; };
-struct Space {
-  CutItem* cut;
-  TokenInfo* tokens;
-  TileParts* tiles;
-  TileParts* prefix_tiles;
-  float* records;
-  int workgroups, hq;
+// A place on the line: an item and where it starts.
+struct Walk {
+  int i, tile;                 // request (-1: the prefix), tile
+  int64_t start, req_start;
+  Items it;
 };
+
+template <Kind K>
+__device__ __forceinline__ Walk item_at(const Requests& r, const PagedAttnArgs& a, const Line& line, int64_t x) {
+  Walk w{-1, 0, 0, 0, prefix_items<K>(r, a)};
+  if (x >= w.it.cost(w.it.tiles)) {
+    const uint64_t at = __builtin_amdgcn_ballot_w64(line.before <= x);
+    const int owner = 63 - __builtin_clzll(at);
+    w.req_start = lane_value(line.before, owner);
+    w.i = owner * line.per;
+    w.it = items_of<K>(r, a, w.i);
+    while (w.req_start + w.it.cost(w.it.tiles) <= x && w.i + 1 < a.n_req) {
+      w.req_start += w.it.cost(w.it.tiles);
+      w.it = items_of<K>(r, a, ++w.i);
+    }
+  }
+  int hi = w.it.tiles - 1;
+  while (w.tile < hi) {
+    const int mid = (w.tile + hi + 1) >> 1;
+    if (w.req_start + w.it.cost(mid) <= x) w.tile = mid; else hi = mid - 1;
+  }
+  w.start = w.req_start + w.it.cost(w.tile);
+  return w;
+}
+
+// The next item; there has to be one.
+template <Kind K>
+__device__ __forceinline__ void next_item(const Requests& r, const PagedAttnArgs& a, Walk& w) {
+  if (++w.tile < w.it.tiles) {
+    w.start = w.req_start + w.it.cost(w.tile);
+    return;
+  }
+  w.req_start += w.it.cost(w.it.tiles);
+  w.start = w.req_start;
+  w.tile = 0;
+  do {
+    w.it = items_of<K>(r, a, ++w.i);
+  } while (w.it.tiles == 0 && w.i + 1 < a.n_req);
+}
+
+// What the launches that join the parts have to know, at the start of the
+// workspace.  Workers of a KV head: its W workgroups for the wide items, its 4 W
+// wavefronts for the narrow ones.  Without a prefix: for each worker, wide ones
+// first, the item that it has begun and the next `parts` ones go on with.  With
+// one, where every row has parts: for each token, for each tile (at the token of its
+// first row) and for each prefix tile the workers w0 .. w0 + n - 1 that go on with it.
+struct CutItem { int row, rows, parts, blind; };   // rows of the batch; the first `blind` see no key
+struct TokenInfo { int j, t, kv, pad; };           // token j of t new ones, kv keys
+struct TileParts { int w0, n; };
 // Their bytes ahead of the records, a multiple of 16.
 __host__ __device__ __forceinline__ int64_t prefix_tiles_most(int64_t tokens, int64_t group) {
   return (tokens * group + kWide - 1) / kWide;
@@ -180,33 +227,22 @@ __host__ __device__ __forceinline__ int64_t prefix_tiles_most(int64_t tokens, in
 __host__ __device__ __forceinline__ int64_t header_bytes(int workgroups, int64_t tokens, int64_t group, bool prefix) {
   return prefix ? (tokens * static_cast<int64_t>(sizeof(TokenInfo) + sizeof(TileParts)) +
                    prefix_tiles_most(tokens, group) * static_cast<int64_t>(sizeof(TileParts)) + 15) / 16 * 16
-                : workgroups * static_cast<int64_t>(sizeof(CutItem));
+                : 5 * workgroups * static_cast<int64_t>(sizeof(CutItem));
 }
+// Rows of records that the workers of one KV head have.
+__host__ __device__ __forceinline__ int64_t worker_rows(int workgroups) { return workgroups * (kWide + 4 * kNarrow); }
 
-// Records, (D + 4) floats a row (D sums, maximum, sum of weights, 2 unused):
-// 128 rows per workgroup and KV head for a part that goes on from the workgroup
-// before, then as many for one that the next goes on with; with a prefix, in place
-// of those, one per row for the first part of the own keys and one for the prefix.
-template <int D>
-__device__ __forceinline__ float* row_record(const Space& s, int64_t row) { return s.records + row * (D + 4); }
-template <int D>
-__device__ __forceinline__ float* going_on(const Space& s, const PagedAttnArgs& a, int w, int head, int row) {
-  return row_record<D>(s, (static_cast<int64_t>(w) * a.hkv + head) * kWide + row);
-}
-template <int D>
-__device__ __forceinline__ float* begun(const Space& s, const PagedAttnArgs& a, int w, int head, int row) {
-  return going_on<D>(s, a, s.workgroups + w, head, row);
-}
-// at: (token, query head) as an element of [tokens][heads].
-template <int D>
-__device__ __forceinline__ float* own_row(const Space& s, const PagedAttnArgs& a, int64_t at) {
-  return row_record<D>(s, static_cast<int64_t>(s.workgroups) * a.hkv * kWide + at);
-}
-template <int D>
-__device__ __forceinline__ float* prefix_row(const Space& s, const PagedAttnArgs& a, int64_t at) {
-  return own_row<D>(s, a, static_cast<int64_t>(a.tokens) * s.hq + at);
-}
-
+// Records, (D + 4) floats a row: D sums, maximum, sum of weights, 2 unused.  For each
+// worker and KV head the rows of a tile that goes on from the worker before; then as
+// many for one that the next goes on with, or, with a prefix, a row per (token,
+// query head) for the first part of the own keys and one for that of the prefix.
+struct Space {
+  CutItem* cut;
+  TokenInfo* tokens;
+  TileParts* tiles;
+  TileParts* prefix_tiles;
+  float* records;
+};
 __device__ __forceinline__ Space space_of(const PagedAttnArgs& a) {
   Space s;
   s.cut = reinterpret_cast<CutItem*>(a.ws);
@@ -214,9 +250,25 @@ __device__ __forceinline__ Space space_of(const PagedAttnArgs& a) {
   s.tiles = reinterpret_cast<TileParts*>(s.tokens + a.tokens);
   s.prefix_tiles = s.tiles + a.tokens;
   s.records = a.ws + header_bytes(a.workgroups, a.tokens, a.group, a.prefix_pages > 0) / 4;
-  s.workgroups = a.workgroups;
-  s.hq = a.hkv * a.group;
   return s;
+}
+template <int D, Kind K>
+__device__ __forceinline__ float* going_on(const Space& s, const PagedAttnArgs& a, int w, int head, int row) {
+  const int64_t first = K == kWideItem ? 0 : static_cast<int64_t>(a.workgroups) * a.hkv * kWide;
+  return s.records + (first + (static_cast<int64_t>(w) * a.hkv + head) * kRows<K> + row) * (D + 4);
+}
+template <int D, Kind K>
+__device__ __forceinline__ float* begun(const Space& s, const PagedAttnArgs& a, int w, int head, int row) {
+  return going_on<D, K>(s, a, w, head, row) + worker_rows(a.workgroups) * a.hkv * (D + 4);
+}
+// at: (token, query head) as an element of [tokens][heads].
+template <int D>
+__device__ __forceinline__ float* own_row(const Space& s, const PagedAttnArgs& a, int64_t at) {
+  return s.records + (worker_rows(a.workgroups) * a.hkv + at) * (D + 4);
+}
+template <int D>
+__device__ __forceinline__ float* prefix_row(const Space& s, const PagedAttnArgs& a, int64_t at) {
+  return own_row<D>(s, a, static_cast<int64_t>(a.tokens) * a.hkv * a.group + at);
 }
 
 // ---------------------------------------------------- one part of one tile
@@ -273,38 +325,31 @@ __device__ __forceinline__ int v_at(int row, int dim) {
   return row * D + (((dim >> 3) ^ v_swizzle<D>(row)) << 3) + (dim & 7);
 }
 
-template <int D>
-struct NarrowLds {
-  union {
-    _Float16 v[4][32 * D];          // a block of V per wavefront
-    float acc[4][16][D + 4];        // the wavefronts' parts
-  };
-  float m[4][16], l[4][16];
-};
+constexpr int kBlock = kKeys<kWideItem>;
 template <int D>
 struct WideLds {
-  _Float16 k[2][kBlockKeys * D], v[2][kBlockKeys * D];   // two blocks: one read, one on its way
+  _Float16 k[2][kBlock * D], v[2][kBlock * D];   // two blocks: one read, one on its way
   int bad;
 };
 template <int D>
 union TileLds {
-  NarrowLds<D> n;
-  WideLds<D> w;
+  _Float16 narrow[4][kKeys<kNarrowItem> * D];            // a block of V per wavefront
+  WideLds<D> wide;
 };
 
-// One tile of 16 rows against the keys [k.lo, k.hi) of one KV head: the four
-// wavefronts take blocks of 32 keys in turn.
+// One tile of 16 rows against the keys [k.lo, k.hi) of one KV head, by one
+// wavefront, 32 keys at a time, the next ones on their way meanwhile:
 //   S^T = K Q^T   16 keys x 16 rows, K fragments straight from their pages,
 //   O^T += V^T W^T, V^T read transposed out of LDS; its k slots are relabelled to
 //   the keys that a lane holds weights of, so the weights never leave their lane.
 // limit: keys visible to this lane's row (lane & 15), 0 for rows that do not
-// exist.  Leaves the joined sums in s.acc[0], maxima in s.m[0], sums in s.l[0].
+// exist.  acc[b][r]: dimension 16 b + 4 (lane / 16) + r of the row; m, l: its maximum
+// and sum of weights.
 template <int D>
-__device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, NarrowLds<D>& s, const uint16_t* q_row, int limit,
-                                            int head, const Keys& k) {
+__device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, _Float16* vl, const uint16_t* q_row, int limit,
+                                            int head, const Keys& k, float4v (&acc)[D / 16], float& m, float& l) {
   constexpr int KS = D / 32, DB = D / 16, VL = D / 16;   // k steps of S, dimension tiles, V loads per lane
-  const int thread = fresh_thread(), lane = thread & 63, col = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+  const int lane = fresh_thread() & 63, col = lane & 15, g = lane >> 4;
   const int page_rows = 1 << a.page_log2;
   int most = limit, least = limit > 0 ? limit : INT32_MAX;
 #pragma unroll
@@ -319,20 +364,26 @@ __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, NarrowLds<D>
   for (int c = 0; c < KS; ++c) qf[c] = *reinterpret_cast<const half8v*>(q_row + 32 * c + 8 * g);
 
   bool bad = false;                                                 // a page id that is none
-  // Row 0 of the page of 16 keys (keys past the end: the last ones), in rows of the pool.
-  auto row_of = [&](int key) __attribute__((always_inline)) {
-    const int t = min(key, (hi - 1) & ~15);
-    int id = k.pages[t >> a.page_log2];
-    if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(a.n_pages)) {
+  // The page ids of 64 times 16 keys are fetched at once, a lane each.
+  const int end = (hi - 1) & ~15;
+  int ids = 0;
+  auto fetch_ids = [&](int key) __attribute__((always_inline)) {
+    ids = k.pages[min(key + 16 * lane, end) >> a.page_log2];
+    if (static_cast<uint32_t>(ids) >= static_cast<uint32_t>(a.n_pages)) {
       bad = true;
-      id = 0;
+      ids = 0;
     }
-    return ((static_cast<int64_t>(id) * a.hkv + head) << a.page_log2) + (t & (page_rows - 1));
+  };
+  // Row of the pools of the first of 16 keys (past the end: the last ones).
+  auto row_of = [&](int key) __attribute__((always_inline)) {
+    const int id = __builtin_amdgcn_readlane(ids, (key - k.lo) >> 4 & 63);
+    return ((static_cast<int64_t>(id) * a.hkv + head) << a.page_log2) + (min(key, end) & (page_rows - 1));
   };
   struct Blk { half8v k[2][KS], v[VL]; };
   auto load = [&](int kb) __attribute__((always_inline)) {
     Blk b;
     int64_t row[2];
+    if (((kb - k.lo) >> 4 & 63) == 0) fetch_ids(kb);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       row[t] = row_of(kb + 16 * t);
@@ -347,18 +398,16 @@ __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, NarrowLds<D>
     }
     return b;
   };
-  float4v acc[DB];
 #pragma unroll
   for (int b = 0; b < DB; ++b) acc[b] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-  float m = -FLT_MAX, l = 0.0f;
+  m = -FLT_MAX;
+  l = 0.0f;
 
-  _Float16* const vl = s.v[wave];
-  const int first = k.lo + 32 * wave;
   Blk cur;
-  if (first < hi) cur = load(first);
-  for (int kb = first; kb < hi; kb += 128) {
+  if (k.lo < hi) cur = load(k.lo);
+  for (int kb = k.lo; kb < hi; kb += 32) {
     const Blk x = cur;
-    if (kb + 128 < hi) cur = load(kb + 128);
+    if (kb + 32 < hi) cur = load(kb + 32);
 #pragma unroll
     for (int j = 0; j < VL; ++j) {
       const int piece = lane + 64 * j;
@@ -440,14 +489,6 @@ __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, NarrowLds<D>
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   if (__builtin_amdgcn_ballot_w64(bad) != 0) l = __builtin_nanf("");
-  __syncthreads();                                          // V has been read by every wavefront
-#pragma unroll
-  for (int b = 0; b < DB; ++b) *reinterpret_cast<float4v*>(&s.acc[wave][col][16 * b + 4 * g]) = acc[b];
-  if (g == 0) {
-    s.m[wave][col] = m;
-    s.l[wave][col] = l;
-  }
-  __syncthreads();
 }
 
 // One tile of 128 rows against the keys [k.lo, hi) of one KV head: wavefront w has
@@ -484,27 +525,37 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
   m = -FLT_MAX;
   l = 0.0f;
 
-  // This wavefront's 16 keys of the block at kb (keys past the end: the last ones).
+  // This wavefront's 16 keys of a block (keys past the end: the last ones).  The page
+  // ids of 64 blocks are fetched at once, a lane each: a load in the loop would wait
+  // for the copies under way.
   const int last = (hi - 1) & ~15;
   bool bad = false;
-  auto page_of = [&](int kb) __attribute__((always_inline)) {
-    return __builtin_amdgcn_readfirstlane(k.pages[min(kb + 16 * wave, last) >> a.page_log2]);
-  };
-  const int lrow = lane / C, chunk = lane % C;            // of a piece: 64 / C rows of C chunks
-  auto copy = [&](int buf, int kb, int id) __attribute__((always_inline)) {
-    if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(a.n_pages)) {
+  int ids = 0;
+  auto fetch_ids = [&](int kb) __attribute__((always_inline)) {
+    ids = k.pages[min(kb + kBlock * lane + 16 * wave, last) >> a.page_log2];
+    if (static_cast<uint32_t>(ids) >= static_cast<uint32_t>(a.n_pages)) {
       bad = true;
-      id = 0;
+      ids = 0;
     }
+  };
+  // Of a piece: 64 / C rows of C chunks; byte offsets from the first row.
+  uint32_t k_off[PIECES], v_off[PIECES];
+#pragma unroll
+  for (int j = 0; j < PIECES; ++j) {
+    const int r = j * (64 / C) + lane / C;
+    k_off[j] = 2 * (r * D + (((lane % C) ^ k_swizzle<D>(r)) << 3));
+    v_off[j] = 2 * (r * D + (((lane % C) ^ v_swizzle<D>(r)) << 3));
+  }
+  auto copy = [&](int buf, int kb) __attribute__((always_inline)) {
+    const int n = (kb - k.lo) / kBlock & 63;
+    if (n == 0) fetch_ids(kb);
+    const int id = __builtin_amdgcn_readlane(ids, n);
     const int t = min(kb + 16 * wave, last) & (page_rows - 1);
     const int64_t row = ((static_cast<int64_t>(id) * a.hkv + head) << a.page_log2) + t;
-    const uint16_t* kr = a.k_pages + row * D;
-    const uint16_t* vr = a.v_pages + row * D;
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-      const int r = j * (64 / C) + lrow;
-      qg::lds_dma16(kr + r * D + ((chunk ^ k_swizzle<D>(r)) << 3), &s.k[buf][16 * wave * D + 512 * j]);
-      qg::lds_dma16(vr + r * D + ((chunk ^ v_swizzle<D>(r)) << 3), &s.v[buf][16 * wave * D + 512 * j]);
+      qg::lds_dma16(a.k_pages + row * D, k_off[j], &s.k[buf][16 * wave * D + 512 * j]);
+      qg::lds_dma16(a.v_pages + row * D, v_off[j], &s.v[buf][16 * wave * D + 512 * j]);
     }
   };
   auto compute = [&](int buf, int kb) __attribute__((always_inline)) {
@@ -523,8 +574,16 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
             *reinterpret_cast<const half8v*>(&kl[(32 * t + col) * D + (((2 * c + lh) ^ k_swizzle<D>(col)) << 3)]);
         st[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, qf[c], st[t], 0, 0, 0);
       }
+    // Fragments a few MFMAs ahead of their use.
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int c = 0; c < 2 * KS - 4; ++c) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     // Lane: row col, keys kb + 32 t + 8 (r / 4) + 4 lh + r % 4.
-    const bool masked = kb + kBlockKeys > all;
+    const bool masked = kb + kBlock > all;
     if (masked) {
       const int seen = min(limit, hi) - kb - 4 * lh;
 #pragma unroll
@@ -573,6 +632,13 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
 #pragma unroll
         for (int b = 0; b < DB; ++b)
           acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(kk, b), w[kk], acc[b], 0, 0, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
+#pragma unroll
+      for (int c = 0; c < 4 * DB - 4; ++c) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
     } else {                                                // as in narrow_part
       bool odd = false;
 #pragma unroll
@@ -581,7 +647,7 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
         for (int b = 0; b < DB; ++b)
           acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(finite_part(value(kk, b), odd), w[kk], acc[b], 0, 0, 0);
       if (__builtin_amdgcn_ballot_w64(odd) != 0) {
-        for (int key = 0; key < kBlockKeys; ++key) {
+        for (int key = 0; key < kBlock; ++key) {
           if (kb + key < min(limit, hi)) {
 #pragma unroll
             for (int b = 0; b < DB; ++b)
@@ -596,10 +662,9 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
     }
   };
   if (k.lo < hi) {
-    copy(0, k.lo, page_of(k.lo));
-    int id = page_of(k.lo + kBlockKeys);
+    copy(0, k.lo);
     int buf = 0;
-    for (int kb = k.lo; kb < hi; kb += kBlockKeys, buf ^= 1) {
+    for (int kb = k.lo; kb < hi; kb += kBlock, buf ^= 1) {
       // This wavefront's copies have landed and its reads of the other block are
       // done; after the barrier so are everybody's.
       asm volatile("" ::: "memory");
@@ -607,19 +672,132 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
       qg::vm_wait<0>();
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (kb + kBlockKeys < hi) {
-        copy(buf ^ 1, kb + kBlockKeys, id);
-        id = page_of(kb + 2 * kBlockKeys);
-      }
+      if (kb + kBlock < hi) copy(buf ^ 1, kb + kBlock);
       if (kb < most) compute(buf, kb);
     }
   }
   __syncthreads();
-  if (bad) s.bad = 1;
+  if (bad) s.bad = 1;                                       // (any lane: an id outside the pool among those fetched)
   __syncthreads();
   const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
   if (s.bad) l = __builtin_nanf("");
+}
+
+// Four dimensions of a row's result: the output, or a part's record.
+template <int D>
+__device__ __forceinline__ void write4(uint16_t* out, float* rec, int dim, float4v v, float inv, bool none) {
+  if (out) {
+    half4v h;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(none ? 0.0f : v[c] * inv);
+    *reinterpret_cast<half4v*>(out + dim) = h;
+  } else {
+    *reinterpret_cast<float4v*>(rec + dim) = v;
+  }
+}
+
+// Worker w's length of the line of kind K.
+template <int D, Kind K>
+__device__ __forceinline__ void work_line(const PagedAttnArgs& a, const Requests& req, const Line& line, TileLds<D>& s,
+                                          int w, int head) {
+  const Space space = space_of(a);
+  const int prefix_len = a.prefix_pages << a.page_log2;
+  const int64_t hq = static_cast<int64_t>(a.hkv) * a.group;
+  const int64_t x0 = w * line.chunk, x1 = min(x0 + line.chunk, line.total);
+  CutItem* const cut = space.cut + (K == kWideItem ? w : a.workgroups + w);
+  const bool teller = head == 0 && (K == kWideItem ? threadIdx.x == 0 : (threadIdx.x & 63) == 0);
+  bool begins = false;                                      // an item that the next worker goes on with
+  if (x0 < line.total) {
+    Walk at = item_at<K>(req, a, line, x0);
+    for (;;) {
+      const bool shared = at.i < 0;
+      const int i = at.i;
+      const int64_t end = at.req_start + at.it.cost(at.tile + 1);
+      const int row0 = at.tile * kRows<K>, last = min(row0 + kRows<K>, at.it.rows) - 1;
+      const int t = shared ? 0 : at.it.rows / a.group;
+      const int seen = shared ? prefix_len : min(req.kv[i], req.kv[i] - t + last / a.group + 1);   // keys of the last row
+      const int first_key = shared ? 0 : prefix_len;
+      const int blocks = blocks_of<K>(seen - first_key), least = a.min_part[K];
+      // Blocks of the item ahead of a place on the line; what would be a very short
+      // part goes to its neighbour.
+      auto ahead = [&](int64_t x) __attribute__((always_inline)) {
+        const int64_t b = x - at.start - a.item_cost[K];
+        return x >= end ? blocks : b < 0 ? 0 : b > blocks - least ? blocks : b < least ? 0 : static_cast<int>(b);
+      };
+      const int from = ahead(x0), to = ahead(x1);
+      if (from < to) {
+        const int thread = fresh_thread(), lane = thread & 63, group_thread = K == kWideItem ? thread : lane;
+        if (from == 0 && head == 0) {
+          // Workers w + 1 .. w + n go on with the item: those whose length begins
+          // `least` blocks or more before its end.
+          const int64_t left = min(at.start + a.item_cost[K] + blocks - least, end - 1) - (w + 1) * line.chunk;
+          const int n = to == blocks ? 0 : static_cast<int>(left / line.chunk) + 1;
+          if (!a.prefix_pages) {
+            // The rows of the batch, those of them that see no key.
+            if (n && group_thread == 0)
+              *cut = CutItem{req.off[i] * a.group + row0, last + 1 - row0, n,
+                             min(max((t - req.kv[i]) * a.group - row0, 0), kWide)};
+            begins = begins || n;
+          } else if (shared) {
+            if (group_thread == 0) space.prefix_tiles[at.tile] = TileParts{w + 1, n};
+          } else {
+            if (group_thread == 0) space.tiles[req.off[i] + row0 / a.group] = TileParts{w + 1, n};
+            // The tokens whose first row is in this tile.
+            for (int j = (row0 + a.group - 1) / a.group + group_thread; j * a.group <= last; j += K == kWideItem ? 256 : 64)
+              space.tokens[req.off[i] + j] = TokenInfo{j, t, req.kv[i], 0};
+          }
+        }
+        const bool whole = !a.prefix_pages && from == 0 && to == blocks;
+        Keys k;
+        k.pages = shared ? a.prefix : a.tables + static_cast<int64_t>(i) * a.max_pages;
+        k.lo = first_key + from * kKeys<K>;
+        k.hi = min(seen, first_key + to * kKeys<K>);
+        // This lane's row of the tile.
+        const int col = K == kWideItem ? (thread >> 6) * 32 + (lane & 31) : lane & 15;
+        const int row = min(row0 + col, last);
+        int token = row / a.group;
+        const int gq = row - token * a.group;
+        const int r = shared ? request_of(req, a.n_req, token) : i;
+        if (!shared) token += req.off[i];
+        const int sees = max(min(req.kv[r], req.kv[r] - max(req.off[r + 1] - token, 0) + 1), 0);
+        const int limit = row0 + col > last ? 0 : shared ? min(sees, prefix_len) : sees;
+        const int64_t el = token * hq + head * a.group + gq;  // of q and out
+        float m, l;
+        float16v wide[D / 32];
+        float4v narrow[D / 16];
+        if constexpr (K == kWideItem) wide_part<D>(a, s.wide, a.q + el * D, limit, head, k, wide, m, l);
+        else narrow_part<D>(a, s.narrow[__builtin_amdgcn_readfirstlane(thread >> 6)], a.q + el * D, limit, head, k, narrow, m, l);
+        if (row0 + col <= last) {
+          uint16_t* const out = whole ? a.out + el * D : nullptr;
+          float* const rec = from ? going_on<D, K>(space, a, w, head, col)
+                             : !a.prefix_pages ? begun<D, K>(space, a, w, head, col)
+                             : shared ? prefix_row<D>(space, a, el) : own_row<D>(space, a, el);
+          const float inv = 1.0f / l;
+          if constexpr (K == kWideItem) {
+            const int lh = lane >> 5;
+#pragma unroll
+            for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+              for (int q = 0; q < 16; q += 4)
+                write4<D>(out, rec, 32 * b + 2 * q + 4 * lh,
+                          float4v{wide[b][q], wide[b][q + 1], wide[b][q + 2], wide[b][q + 3]}, inv, sees == 0);
+          } else {
+#pragma unroll
+            for (int b = 0; b < D / 16; ++b) write4<D>(out, rec, 16 * b + 4 * (lane >> 4), narrow[b], inv, sees == 0);
+          }
+          if (!whole && lane < (K == kWideItem ? 32 : 16)) {
+            rec[D] = m;
+            rec[D + 1] = l;
+          }
+        }
+        if (K == kWideItem) __syncthreads();                // the tile's LDS is free
+      }
+      if (end >= x1) break;
+      next_item<K>(req, a, at);
+    }
+  }
+  if (!a.prefix_pages && !begins && teller) cut->parts = 0;
 }
 
 // Workgroups that a CU holds at once, by registers and LDS.
@@ -631,185 +809,21 @@ __global__ __launch_bounds__(256, kResident<D>) void paged_attn_kernel(PagedAttn
   __shared__ Requests req;
   __shared__ __attribute__((aligned(1024))) TileLds<D> s;
   load_requests(req, a);
-  const Line line = make_line(req, a);
-  const Space space = space_of(a);
   const int head = static_cast<int>(blockIdx.x % a.hkv), wg = static_cast<int>(blockIdx.x / a.hkv);
-  const int64_t x0 = wg * line.chunk, x1 = min(x0 + line.chunk, line.total);   // this workgroup's length of the line
-  bool begins = false;                                      // an item that the next workgroup goes on with
-  if (x0 >= line.total) {
-    if (!a.prefix_pages && head == 0 && threadIdx.x == 0) space.cut[wg].parts = 0;
-    return;
-  }
-  const int prefix_len = a.prefix_pages << a.page_log2;
-  const int64_t hq = space.hq;
-  // The item at x0: a prefix tile, or a request and a tile of it; it starts at `start`.
-  const int64_t prefix_end = static_cast<int64_t>(line.prefix_tiles) * line.prefix_cost;
-  int i = -1, tile = 0;                                     // request (-1: the prefix), tile
-  int64_t start = 0, req_start = prefix_end;
-  Items it{line.prefix_rows, line.prefix_tile, line.prefix_tiles, line.prefix_cost, 0};
-  if (x0 < prefix_end) {
-    tile = static_cast<int>(static_cast<double>(x0) / line.prefix_cost);
-    tile -= it.cost(tile) > x0;
-    tile += it.cost(tile + 1) <= x0;
-    start = it.cost(tile);
-  } else {
-    const uint64_t at = __builtin_amdgcn_ballot_w64(line.before <= x0);
-    const int owner = 63 - __builtin_clzll(at);
-    req_start = lane_value(line.before, owner);
-    i = owner * line.per;
-    it = items_of(req, a, i);
-    while (req_start + it.cost(it.tiles) <= x0 && i + 1 < a.n_req) {
-      req_start += it.cost(it.tiles);
-      it = items_of(req, a, ++i);
-    }
-    int hi = it.tiles - 1;
-    while (tile < hi) {
-      const int mid = (tile + hi + 1) >> 1;
-      if (req_start + it.cost(mid) <= x0) tile = mid; else hi = mid - 1;
-    }
-    start = req_start + it.cost(tile);
-  }
-  for (;;) {
-    const bool shared = i < 0;
-    const int64_t end = (shared ? 0 : req_start) + it.cost(tile + 1);
-    const int row0 = tile * it.per, rows = it.rows, per = it.per;
-    const int last = min(row0 + per, rows) - 1, t = shared ? 0 : rows / a.group;
-    const int seen = shared ? prefix_len : min(req.kv[i], req.kv[i] - t + last / a.group + 1);   // keys of the last row
-    const int first_key = shared ? 0 : prefix_len;
-    const int blocks = blocks_of(seen - first_key);
-    // Blocks of the item ahead of a place on the line; what would be a very short
-    // part goes to its neighbour.
-    const Cost cost = cost_of(a, per);
-    const int min_part = per == kWide ? a.wide_part : a.narrow_part;
-    auto ahead = [&](int64_t x) __attribute__((always_inline)) {
-      const int64_t keys = max<int64_t>(min<int64_t>(x - start - cost.item, INT32_MAX), -1);
-      const int b = static_cast<int>(keys) / cost.block;
-      return x >= end ? blocks : keys < 0 ? 0 : b > blocks - min_part ? blocks : b < min_part ? 0 : b;
-    };
-    const int from = ahead(x0), to = ahead(x1);
-    if (from < to) {
-      const int thread = fresh_thread(), lane = thread & 63;
-      if (from == 0 && head == 0) {
-        // Workgroups wg + 1 .. wg + n go on with the item: those whose length begins
-        // at the block blocks - min_part or before.
-        const int64_t left =
-            min(start + cost.item + static_cast<int64_t>(blocks - min_part + 1) * cost.block, end) - 1 - (wg + 1) * line.chunk;
-        const int n = to == blocks ? 0 : static_cast<int>(left / line.chunk) + 1;
-        if (!a.prefix_pages) {
-          // The rows of the batch, those of them that see no key.
-          if (n && thread == 0)
-            space.cut[wg] = CutItem{req.off[i] * a.group + row0, last + 1 - row0, n,
-                                    min(max((t - req.kv[i]) * a.group - row0, 0), kWide)};
-          begins = begins || n;
-        } else if (shared) {
-          if (thread == 0) space.prefix_tiles[tile] = TileParts{wg + 1, n};
-        } else {
-          if (thread == 0) space.tiles[req.off[i] + row0 / a.group] = TileParts{wg + 1, n};
-          // The tokens whose first row is in this tile.
-          for (int j = (row0 + a.group - 1) / a.group + thread; j * a.group <= last; j += 256)
-            space.tokens[req.off[i] + j] = TokenInfo{j, t, req.kv[i], per};
-        }
-      }
-      const bool whole = !a.prefix_pages && from == 0 && to == blocks;
-      Keys k;
-      k.pages = shared ? a.prefix : a.tables + static_cast<int64_t>(i) * a.max_pages;
-      k.lo = first_key + from * kBlockKeys;
-      k.hi = min(seen, first_key + to * kBlockKeys);
-      // This lane's row of the tile.
-      const bool narrow = per == kNarrow;
-      const int col = narrow ? lane & 15 : (thread >> 6) * 32 + (lane & 31);
-      const int row = min(row0 + col, last);
-      int token = row / a.group;
-      const int gq = row % a.group;
-      const int r = shared ? request_of(req, a.n_req, token) : i;
-      if (!shared) token += req.off[i];
-      const int sees = max(min(req.kv[r], req.kv[r] - max(req.off[r + 1] - token, 0) + 1), 0);
-      const int limit = row0 + col > last ? 0 : shared ? min(sees, prefix_len) : sees;
-      const int64_t at = token * hq + head * a.group + gq;  // of q and out
-      if (!narrow) {
-        float16v acc[D / 32];
-        float m, l;
-        wide_part<D>(a, s.w, a.q + at * D, limit, head, k, acc, m, l);
-        const int lh = lane >> 5;
-        if (row0 + col <= last) {
-          if (whole) {
-            const float inv = sees ? 1.0f / l : 0.0f;
-            uint16_t* o = a.out + at * D;
-#pragma unroll
-            for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-              for (int q = 0; q < 16; q += 4) {
-                half4v h;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(sees ? acc[b][q + c] * inv : 0.0f);
-                *reinterpret_cast<half4v*>(o + 32 * b + 2 * q + 4 * lh) = h;
-              }
-          } else {
-            float* rec = from ? going_on<D>(space, a, wg, head, col)
-                         : !a.prefix_pages ? begun<D>(space, a, wg, head, col)
-                         : shared ? prefix_row<D>(space, a, at) : own_row<D>(space, a, at);
-#pragma unroll
-            for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-              for (int q = 0; q < 16; q += 4)
-                *reinterpret_cast<float4v*>(rec + 32 * b + 2 * q + 4 * lh) =
-                    float4v{acc[b][q], acc[b][q + 1], acc[b][q + 2], acc[b][q + 3]};
-            if (lh == 0) {
-              rec[D] = m;
-              rec[D + 1] = l;
-            }
-          }
-        }
-      } else {
-        narrow_part<D>(a, s.n, a.q + at * D, limit, head, k);
-        // The four wavefronts' sums, joined; thread: row, 4 dimensions.
-        for (int e = thread; e < 16 * (D / 4); e += 256) {
-          const int x = e / (D / 4), d4 = e % (D / 4);
-          if (row0 + x > last) continue;
-          const float mx = fmaxf(fmaxf(s.n.m[0][x], s.n.m[1][x]), fmaxf(s.n.m[2][x], s.n.m[3][x]));
-          float4v o{0.0f, 0.0f, 0.0f, 0.0f};
-          float l = 0.0f;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float f = __builtin_amdgcn_exp2f(s.n.m[w][x] - mx);
-            l = fmaf(s.n.l[w][x], f, l);
-            const float4v v = *reinterpret_cast<const float4v*>(&s.n.acc[w][x][4 * d4]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) o[c] = fmaf(v[c], f, o[c]);
-          }
-          const int tk = (row0 + x) / a.group;              // of the request or the batch
-          const int64_t xat = ((shared ? 0 : req.off[i]) + tk) * hq + head * a.group + (row0 + x) % a.group;
-          if (whole) {
-            const bool none = req.kv[i] - t + tk + 1 <= 0;
-            half4v h;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) h[c] = static_cast<_Float16>(none ? 0.0f : o[c] / l);
-            *reinterpret_cast<half4v*>(a.out + xat * D + 4 * d4) = h;
-          } else {
-            float* rec = from ? going_on<D>(space, a, wg, head, x)
-                         : !a.prefix_pages ? begun<D>(space, a, wg, head, x)
-                         : shared ? prefix_row<D>(space, a, xat) : own_row<D>(space, a, xat);
-            *reinterpret_cast<float4v*>(rec + 4 * d4) = o;
-            if (d4 == 0) {
-              rec[D] = mx;
-              rec[D + 1] = l;
-            }
-          }
-        }
-      }
-      __syncthreads();                                      // the tile's LDS is free
-    }
-    if (end >= x1) break;
-    start = end;
-    if (++tile == it.tiles) {
-      req_start = end;
-      tile = 0;
-      do {                                                  // (there is one: end < x1 <= total)
-        it = items_of(req, a, ++i);
-      } while (it.tiles == 0 && i + 1 < a.n_req);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // A CU holds workgroups of both halves of the grid.  Where there are fewer narrow
+  // lengths than wavefronts, they go to the last workgroups, the wide ones to the first.
+  const int narrow_first = 2 * blockIdx.x >= gridDim.x;
+  for (int phase = 0; phase < 2; ++phase) {
+    if (phase == narrow_first) {
+      const Line line = make_line<kWideItem>(req, a);
+      work_line<D, kWideItem>(a, req, line, s, wg, head);
+    } else {
+      const Line line = make_line<kNarrowItem>(req, a);
+      work_line<D, kNarrowItem>(a, req, line, s, 4 * (a.workgroups - 1 - wg) + wave, head);
+      __syncthreads();                                      // the wide tiles' LDS is free
     }
   }
-  if (!a.prefix_pages && !begins && head == 0 && threadIdx.x == 0) space.cut[wg].parts = 0;
 }
 
 // Parts s0, s0 + step, ... of a row, each with its weight relative to the largest
@@ -886,13 +900,12 @@ __device__ __forceinline__ int64_t element_of(const PagedAttnArgs& a, int row, i
 // Without a prefix: the items that are cut, a workgroup for 16 rows of each.  A row
 // has D / 4 threads, four dimensions each; with few rows several groups of threads
 // share its parts.
-template <int D>
-__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
+template <int D, Kind K>
+__device__ __forceinline__ void join_cut(const PagedAttnArgs& a, int w, int row0, int head) {
   constexpr int C4 = D / 4;
   const Space space = space_of(a);
-  const int head = static_cast<int>(blockIdx.x % a.hkv), rest = static_cast<int>(blockIdx.x / a.hkv);
-  const int w = rest % a.workgroups, row0 = rest / a.workgroups * 16;
-  const CutItem it = space.cut[w];
+  const int workers = K == kWideItem ? a.workgroups : 4 * a.workgroups;
+  const CutItem it = space.cut[K == kWideItem ? w : a.workgroups + w];
   const int rows = min(it.rows - row0, 16);
   if (it.parts == 0 || rows <= 0) return;
   int groups = 1;
@@ -901,13 +914,21 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
   for (int e = threadIdx.x % width; e < rows * C4 || groups > 1; e += width) {   // (once where there are several groups)
     const int row = row0 + min(e / C4, rows - 1), d4 = e % C4;
     auto rec = [&](int x) __attribute__((always_inline)) {
-      return x == 0 ? begun<D>(space, a, w, head, row) : going_on<D>(space, a, min(w + x, a.workgroups - 1), head, row);
+      return x == 0 ? begun<D, K>(space, a, w, head, row) : going_on<D, K>(space, a, min(w + x, workers - 1), head, row);
     };
     Joined r = join_parts<D>(grp, groups, it.parts + 1, d4, rec);
     if (groups > 1) r = join_groups(r, groups, width);
     if (grp == 0 && e < rows * C4) write_joined<D>(a, element_of(a, it.row + row, head), d4, r, row < it.blind);
     if (groups > 1) break;
   }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
+  const int head = static_cast<int>(blockIdx.x % a.hkv), x = static_cast<int>(blockIdx.x / a.hkv);
+  const int narrow = 4 * a.workgroups;
+  if (x < narrow) join_cut<D, kNarrowItem>(a, x, 0, head);
+  else join_cut<D, kWideItem>(a, (x - narrow) % a.workgroups, (x - narrow) / a.workgroups * 16, head);
 }
 
 // With a prefix every row has parts: a workgroup of `groups` groups takes
@@ -921,23 +942,26 @@ __global__ __launch_bounds__(256) void paged_attn_join_rows_kernel(PagedAttnArgs
   const int width = 256 / groups, grp = threadIdx.x / width, th = threadIdx.x % width;
   const int row = static_cast<int>(blockIdx.x / a.hkv) * (width / C4) + th / C4, d4 = th % C4;
   if (row - th / C4 >= rows) return;                        // whole workgroup
-  const int token = min(row, rows - 1) / a.group, gq = min(row, rows - 1) - token * a.group;
+  const int prow = min(row, rows - 1), token = prow / a.group, gq = prow - token * a.group;
   const TokenInfo tp = space.tokens[token];
   // (The test holds whatever lies there for a token of no request, where offsets do not rise.)
-  const bool there = row < rows && (tp.per == kNarrow || tp.per == kWide) && tp.j >= 0 && tp.j <= token;
-  const int per = there ? tp.per : kNarrow, own_row_at = there ? tp.j * a.group + gq : 0;   // row of the request
-  const int tile = own_row_at / per, prefix_tile = tile_rows(rows), prow = token * a.group + gq;
-  const TileParts own = space.tiles[there ? token - tp.j + tile * per / a.group : 0];
-  const TileParts pre = space.prefix_tiles[prow / prefix_tile];
+  const bool there = row < rows && tp.j >= 0 && tp.j <= token && tp.t > tp.j && tp.t <= a.tokens;
+  const int own = there ? tp.j * a.group + gq : 0;          // row of the request
+  const int per = tile_rows(there ? tp.t * a.group : 0), prefix_per = tile_rows(rows);
+  const TileParts op = space.tiles[there ? token - tp.j + own / per * per / a.group : 0];
+  const TileParts pp = space.prefix_tiles[prow / prefix_per];
   const int64_t at = element_of(a, prow, head);
-  const int own_at = min(max(pre.n, 0), a.workgroups) + 1;  // parts of the prefix
-  const int parts = own_at + 1 + min(max(own.n, 0), a.workgroups);
+  const int own_at = min(max(pp.n, 0), 4 * a.workgroups) + 1;   // parts of the prefix
+  const int parts = own_at + 1 + min(max(op.n, 0), 4 * a.workgroups);
+  auto on = [&](int w, int rows_per, int r) __attribute__((always_inline)) {
+    return rows_per == kWide ? going_on<D, kWideItem>(space, a, min(max(w, 0), a.workgroups - 1), head, r % kWide)
+                             : going_on<D, kNarrowItem>(space, a, min(max(w, 0), 4 * a.workgroups - 1), head, r % kNarrow);
+  };
   auto rec = [&](int x) __attribute__((always_inline)) {
-    auto held = [&](int w) __attribute__((always_inline)) { return min(max(w, 0), a.workgroups - 1); };
     if (x == 0) return prefix_row<D>(space, a, at);
-    if (x < own_at) return going_on<D>(space, a, held(pre.w0 + x - 1), head, prow % prefix_tile);
+    if (x < own_at) return on(pp.w0 + x - 1, prefix_per, prow);
     if (x == own_at) return own_row<D>(space, a, at);
-    return going_on<D>(space, a, held(own.w0 + x - own_at - 1), head, own_row_at % per);
+    return on(op.w0 + x - own_at - 1, per, own);
   };
   Joined r = join_parts<D>(grp, groups, there ? parts : 0, d4, rec);
   if (groups > 1) r = join_groups(r, groups, width);
@@ -953,7 +977,7 @@ int workgroups_of(int hkv, int d, int cu_count) {
 
 size_t attn_paged_workspace_bytes(int32_t hq, int32_t hkv, int32_t d, int64_t tokens, bool prefix, int cu_count) {
   const int workgroups = workgroups_of(hkv, d, cu_count);
-  const int64_t slots = static_cast<int64_t>(workgroups) * hkv * kWide;
+  const int64_t slots = worker_rows(workgroups) * hkv;
   const int64_t records = prefix ? slots + 2 * tokens * hq : 2 * slots;
   return static_cast<size_t>(header_bytes(workgroups, tokens, hq / hkv, prefix)) +
          static_cast<size_t>(records) * (d + 4) * sizeof(float);
@@ -967,7 +991,7 @@ hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (!a.prefix_pages) {
-    hipLaunchKernelGGL(paged_attn_join_kernel<D>, dim3(static_cast<unsigned>(a.workgroups * a.hkv * (kWide / 16))), dim3(256),
+    hipLaunchKernelGGL(paged_attn_join_kernel<D>, dim3(static_cast<unsigned>(a.workgroups * a.hkv * (kWide / 16 + 4))), dim3(256),
                        0, st, a);
     return hipGetLastError();
   }
@@ -985,15 +1009,17 @@ hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
 hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, int cu_count, hipStream_t st) {
   if (a.tokens == 0) return hipSuccess;
   a.workgroups = workgroups_of(a.hkv, d, cu_count);
-  a.per_workgroup = 1.0 / a.workgroups;
-  a.narrow_item = 1;
-  a.wide_item = 4;
-  a.wide_block = 2;
-  a.min_chunk = 4;
-  a.narrow_part = 2;
-  a.wide_part = 4;
+  a.per_worker[kWideItem] = 1.0 / a.workgroups;
+  a.per_worker[kNarrowItem] = 0.25 / a.workgroups;
+  a.item_cost[kNarrowItem] = 1;
+  a.item_cost[kWideItem] = 2;
+  a.min_chunk[kNarrowItem] = 2;
+  a.min_chunk[kWideItem] = 4;
+  a.min_part[kNarrowItem] = 1;
+  a.min_part[kWideItem] = 3;
   if (const char* e = tuning_override("QM_PAGED_PLAN"))
-    std::sscanf(e, "%d,%d,%d,%d,%d,%d", &a.narrow_item, &a.wide_item, &a.wide_block, &a.min_chunk, &a.narrow_part, &a.wide_part);
+    std::sscanf(e, "%d,%d,%d,%d,%d,%d", &a.item_cost[0], &a.item_cost[1], &a.min_chunk[0], &a.min_chunk[1], &a.min_part[0],
+                &a.min_part[1]);
   return d == 64 ? launch_paged<64>(a, st) : launch_paged<128>(a, st);
 }
 

@@ -253,11 +253,11 @@ struct PagedAttnArgs {
   float* ws;
   float scale_log2;
   int n_req, tokens, hkv, group, page_log2, max_pages, n_pages, prefix_pages;
-  // Set by the launch: workgroups per KV head (and one over it); costs of an item
-  // beside its keys and of 64 keys for a 128-row tile, in what 64 keys of a 16-row
-  // tile cost; the least that a workgroup takes; the fewest 64-key blocks of a part.
-  double per_workgroup;
-  int workgroups, narrow_item, wide_item, wide_block, min_chunk, narrow_part, wide_part;
+  // Set by the launch: workgroups per KV head; for narrow and wide items, one over
+  // the workers per KV head, the cost of an item beside its keys, the least that a
+  // worker takes, the fewest blocks of a part, in blocks of 32 and of 64 keys.
+  double per_worker[2];
+  int workgroups, item_cost[2], min_chunk[2], min_part[2];
 };
 size_t attn_paged_workspace_bytes(int32_t hq, int32_t hkv, int32_t d, int64_t tokens, bool prefix, int cu_count);
 hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, int cu_count, hipStream_t st);
