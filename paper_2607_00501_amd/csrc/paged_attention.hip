@@ -163,6 +163,13 @@ __device__ __forceinline__ Line make_line(const Requests& r, const PagedAttnArgs
   n.before = prefix + upto - cost;
   n.total = prefix + lane_value(upto, 63);
   n.chunk = max<int64_t>(static_cast<int64_t>(static_cast<double>(n.total) * a.per_worker[K]) + 1, a.min_chunk[K]);
+  if (shared.tiles > 1 && n.chunk < shared.base && shared.base < INT32_MAX) {
+    // Tiles of the prefix cut at the same keys are read at the same time, once from
+    // HBM for all of them: lengths up to 1/8 longer are taken for that.
+    const int whole = static_cast<int>(shared.base), pieces = whole / static_cast<int>(n.chunk);
+    const int64_t even = (whole + pieces - 1) / pieces;
+    if (8 * (even - n.chunk) <= n.chunk) n.chunk = even;
+  }
   return n;
 }
 
@@ -332,8 +339,12 @@ struct WideLds {
   int bad;
 };
 template <int D>
+struct NarrowLds {
+  _Float16 v[4][kKeys<kNarrowItem> * D];                 // a block of V per wavefront
+};
+template <int D>
 union TileLds {
-  _Float16 narrow[4][kKeys<kNarrowItem> * D];            // a block of V per wavefront
+  NarrowLds<D> narrow;
   WideLds<D> wide;
 };
 
@@ -698,9 +709,9 @@ __device__ __forceinline__ void write4(uint16_t* out, float* rec, int dim, float
 }
 
 // Worker w's length of the line of kind K.
-template <int D, Kind K>
-__device__ __forceinline__ void work_line(const PagedAttnArgs& a, const Requests& req, const Line& line, TileLds<D>& s,
-                                          int w, int head) {
+template <int D, Kind K, class Lds>
+__device__ __forceinline__ void work_line(const PagedAttnArgs& a, const Requests& req, const Line& line, Lds& s, int w,
+                                          int head) {
   const Space space = space_of(a);
   const int prefix_len = a.prefix_pages << a.page_log2;
   const int64_t hq = static_cast<int64_t>(a.hkv) * a.group;
@@ -766,8 +777,8 @@ __device__ __forceinline__ void work_line(const PagedAttnArgs& a, const Requests
         float m, l;
         float16v wide[D / 32];
         float4v narrow[D / 16];
-        if constexpr (K == kWideItem) wide_part<D>(a, s.wide, a.q + el * D, limit, head, k, wide, m, l);
-        else narrow_part<D>(a, s.narrow[__builtin_amdgcn_readfirstlane(thread >> 6)], a.q + el * D, limit, head, k, narrow, m, l);
+        if constexpr (K == kWideItem) wide_part<D>(a, s, a.q + el * D, limit, head, k, wide, m, l);
+        else narrow_part<D>(a, s.v[__builtin_amdgcn_readfirstlane(thread >> 6)], a.q + el * D, limit, head, k, narrow, m, l);
         if (row0 + col <= last) {
           uint16_t* const out = whole ? a.out + el * D : nullptr;
           float* const rec = from ? going_on<D, K>(space, a, w, head, col)
@@ -817,49 +828,62 @@ __global__ __launch_bounds__(256, kResident<D>) void paged_attn_kernel(PagedAttn
   for (int phase = 0; phase < 2; ++phase) {
     if (phase == narrow_first) {
       const Line line = make_line<kWideItem>(req, a);
-      work_line<D, kWideItem>(a, req, line, s, wg, head);
+      work_line<D, kWideItem>(a, req, line, s.wide, wg, head);
     } else {
       const Line line = make_line<kNarrowItem>(req, a);
-      work_line<D, kNarrowItem>(a, req, line, s, 4 * (a.workgroups - 1 - wg) + wave, head);
+      work_line<D, kNarrowItem>(a, req, line, s.narrow, 4 * (a.workgroups - 1 - wg) + wave, head);
       __syncthreads();                                      // the wide tiles' LDS is free
     }
   }
 }
 
+// The same where all items are narrow: less LDS to wait for, nothing of the wide ones.
+template <int D>
+__global__ __launch_bounds__(256, kResident<D>) void paged_attn_narrow_kernel(PagedAttnArgs a) {
+  __shared__ Requests req;
+  __shared__ __attribute__((aligned(1024))) NarrowLds<D> s;
+  load_requests(req, a);
+  const int head = static_cast<int>(blockIdx.x % a.hkv), wg = static_cast<int>(blockIdx.x / a.hkv);
+  work_line<D, kNarrowItem>(a, req, make_line<kNarrowItem>(req, a), s,
+                            4 * wg + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head);
+}
+
 // Parts s0, s0 + step, ... of a row, each with its weight relative to the largest
 // maximum so far; rec(s): the record of part s, d4: this thread's four dimensions.
 struct Joined { float4v o; float m, l; };
+template <int D, int BATCH, class Rec>                      // BATCH: records on their way at once
+__device__ __forceinline__ void join_batch(Joined& r, int s0, int step, int parts, int d4, Rec rec) {
+  float4v v[BATCH];
+  float ms[BATCH], ls[BATCH];
+#pragma unroll
+  for (int b = 0; b < BATCH; ++b) {
+    const float* p = rec(min(s0 + b * step, parts - 1));
+    v[b] = *reinterpret_cast<const float4v*>(p + 4 * d4);
+    ms[b] = p[D];
+    ls[b] = p[D + 1];
+  }
+  float mn = r.m;
+#pragma unroll
+  for (int b = 0; b < BATCH; ++b) mn = fmaxf(mn, ms[b]);
+  const float f0 = __builtin_amdgcn_exp2f(r.m - mn);
+  r.m = mn;
+  r.l *= f0;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) r.o[c] *= f0;
+#pragma unroll
+  for (int b = 0; b < BATCH; ++b) {
+    if (s0 + b * step >= parts) continue;
+    const float f = __builtin_amdgcn_exp2f(ms[b] - mn);
+    r.l = fmaf(ls[b], f, r.l);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) r.o[c] = fmaf(v[b][c], f, r.o[c]);
+  }
+}
 template <int D, class Rec>
 __device__ __forceinline__ Joined join_parts(int s0, int step, int parts, int d4, Rec rec) {
-  constexpr int BATCH = 8;                                  // loads in flight
   Joined r{float4v{0.0f, 0.0f, 0.0f, 0.0f}, -FLT_MAX, 0.0f};
-  for (; s0 < parts; s0 += BATCH * step) {
-    float4v v[BATCH];
-    float ms[BATCH], ls[BATCH];
-#pragma unroll
-    for (int b = 0; b < BATCH; ++b) {
-      const float* p = rec(min(s0 + b * step, parts - 1));
-      v[b] = *reinterpret_cast<const float4v*>(p + 4 * d4);
-      ms[b] = p[D];
-      ls[b] = p[D + 1];
-    }
-    float mn = r.m;
-#pragma unroll
-    for (int b = 0; b < BATCH; ++b) mn = fmaxf(mn, ms[b]);
-    const float f0 = __builtin_amdgcn_exp2f(r.m - mn);
-    r.m = mn;
-    r.l *= f0;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) r.o[c] *= f0;
-#pragma unroll
-    for (int b = 0; b < BATCH; ++b) {
-      if (s0 + b * step >= parts) continue;
-      const float f = __builtin_amdgcn_exp2f(ms[b] - mn);
-      r.l = fmaf(ls[b], f, r.l);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) r.o[c] = fmaf(v[b][c], f, r.o[c]);
-    }
-  }
+  for (; parts - s0 > 4 * step; s0 += 12 * step) join_batch<D, 12>(r, s0, step, parts, d4, rec);
+  if (s0 < parts) join_batch<D, 4>(r, s0, step, parts, d4, rec);
   return r;
 }
 
@@ -897,38 +921,70 @@ __device__ __forceinline__ int64_t element_of(const PagedAttnArgs& a, int row, i
   return static_cast<int64_t>(token) * a.hkv * a.group + head * a.group + (row - token * a.group);
 }
 
-// Without a prefix: the items that are cut, a workgroup for 16 rows of each.  A row
-// has D / 4 threads, four dimensions each; with few rows several groups of threads
-// share its parts.
-template <int D, Kind K>
-__device__ __forceinline__ void join_cut(const PagedAttnArgs& a, int w, int row0, int head) {
+// Without a prefix: the items that are cut.  A row has D / 4 threads, four dimensions
+// each.  A workgroup takes the narrow items that four workers have begun, a wavefront
+// each, or all threads for one that has many parts, groups of them sharing the parts;
+// or 32 rows of a wide item.  (A workgroup for every possible item and few rows left
+// thousands without work: 9.4 us against 4.7 for 16 sequences of 1,000 keys, 16 / 8
+// heads of 128.)  QUARTERS: 4 where the batch has 16 rows at most and so few items,
+// of many parts: four workgroups for each, a quarter of the dimensions each (one
+// sequence of 32,000 keys, 250 parts: 11.4 -> 8.0 us).
+constexpr int kManyParts = 8, kJoinRows = 32;
+
+template <int D, int QUARTERS>
+__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
   constexpr int C4 = D / 4;
   const Space space = space_of(a);
-  const int workers = K == kWideItem ? a.workgroups : 4 * a.workgroups;
-  const CutItem it = space.cut[K == kWideItem ? w : a.workgroups + w];
-  const int rows = min(it.rows - row0, 16);
-  if (it.parts == 0 || rows <= 0) return;
-  int groups = 1;
-  while (2 * groups * rows * C4 <= 256 && 2 * groups <= it.parts) groups *= 2;
-  const int width = 256 / groups, grp = threadIdx.x / width;
-  for (int e = threadIdx.x % width; e < rows * C4 || groups > 1; e += width) {   // (once where there are several groups)
-    const int row = row0 + min(e / C4, rows - 1), d4 = e % C4;
-    auto rec = [&](int x) __attribute__((always_inline)) {
-      return x == 0 ? begun<D, K>(space, a, w, head, row) : going_on<D, K>(space, a, min(w + x, workers - 1), head, row);
-    };
-    Joined r = join_parts<D>(grp, groups, it.parts + 1, d4, rec);
-    if (groups > 1) r = join_groups(r, groups, width);
-    if (grp == 0 && e < rows * C4) write_joined<D>(a, element_of(a, it.row + row, head), d4, r, row < it.blind);
-    if (groups > 1) break;
-  }
-}
-
-template <int D>
-__global__ __launch_bounds__(256) void paged_attn_join_kernel(PagedAttnArgs a) {
   const int head = static_cast<int>(blockIdx.x % a.hkv), x = static_cast<int>(blockIdx.x / a.hkv);
-  const int narrow = 4 * a.workgroups;
-  if (x < narrow) join_cut<D, kNarrowItem>(a, x, 0, head);
-  else join_cut<D, kWideItem>(a, (x - narrow) % a.workgroups, (x - narrow) / a.workgroups * 16, head);
+  if (x < QUARTERS * a.workgroups) {
+    const int wg = x % a.workgroups, quarter = x / a.workgroups;
+    CutItem its[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) its[i] = space.cut[a.workgroups + 4 * wg + i];
+    auto rec_of = [&](int w, int row) __attribute__((always_inline)) {
+      return [&space, &a, w, head, row](int part) __attribute__((always_inline)) {
+        return part == 0 ? begun<D, kNarrowItem>(space, a, w, head, row)
+                         : going_on<D, kNarrowItem>(space, a, min(w + part, 4 * a.workgroups - 1), head, row);
+      };
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const CutItem it = its[i];
+      if (it.parts <= kManyParts) continue;
+      constexpr int Q4 = C4 / QUARTERS;
+      int groups = 1;
+      while (2 * groups * it.rows * Q4 <= 256) groups *= 2;
+      const int width = 256 / groups, grp = threadIdx.x / width;
+      for (int e0 = 0; e0 < it.rows * Q4; e0 += width) {    // (once where there are several groups)
+        const int e = e0 + threadIdx.x % width, row = min(e / Q4, it.rows - 1), d4 = quarter * Q4 + e % Q4;
+        Joined r = join_parts<D>(grp, groups, it.parts + 1, d4, rec_of(4 * wg + i, row));
+        if (groups > 1) r = join_groups(r, groups, width);
+        if (grp == 0 && e < it.rows * Q4) write_joined<D>(a, element_of(a, it.row + row, head), d4, r, row < it.blind);
+      }
+      __syncthreads();                                      // (the next item's groups)
+    }
+    if (quarter) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const CutItem it = space.cut[a.workgroups + 4 * wg + wave];
+    if (it.parts == 0 || it.parts > kManyParts) return;
+    for (int e = threadIdx.x & 63; e < it.rows * C4; e += 64) {
+      const int row = e / C4, d4 = e % C4;
+      write_joined<D>(a, element_of(a, it.row + row, head), d4,
+                      join_parts<D>(0, 1, it.parts + 1, d4, rec_of(4 * wg + wave, row)), row < it.blind);
+    }
+  } else {
+    const int w = x % a.workgroups, row0 = (x / a.workgroups - QUARTERS) * kJoinRows;
+    const CutItem it = space.cut[w];
+    if (it.parts == 0) return;
+    for (int e = threadIdx.x; e < min(it.rows - row0, kJoinRows) * C4; e += 256) {
+      const int row = row0 + e / C4, d4 = e % C4;
+      auto rec = [&](int part) __attribute__((always_inline)) {
+        return part == 0 ? begun<D, kWideItem>(space, a, w, head, row)
+                         : going_on<D, kWideItem>(space, a, min(w + part, a.workgroups - 1), head, row);
+      };
+      write_joined<D>(a, element_of(a, it.row + row, head), d4, join_parts<D>(0, 1, it.parts + 1, d4, rec), row < it.blind);
+    }
+  }
 }
 
 // With a prefix every row has parts: a workgroup of `groups` groups takes
@@ -987,12 +1043,15 @@ namespace {
 
 template <int D>
 hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(paged_attn_kernel<D>, dim3(static_cast<unsigned>(a.workgroups * a.hkv)), dim3(256), 0, st, a);
+  const bool narrow = static_cast<int64_t>(a.tokens) * a.group <= kNarrow;
+  const unsigned workgroups = static_cast<unsigned>(a.workgroups * a.hkv);
+  if (narrow) hipLaunchKernelGGL(paged_attn_narrow_kernel<D>, dim3(workgroups), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(paged_attn_kernel<D>, dim3(workgroups), dim3(256), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (!a.prefix_pages) {
-    hipLaunchKernelGGL(paged_attn_join_kernel<D>, dim3(static_cast<unsigned>(a.workgroups * a.hkv * (kWide / 16 + 4))), dim3(256),
-                       0, st, a);
+    if (narrow) hipLaunchKernelGGL((paged_attn_join_kernel<D, 4>), dim3(workgroups * 4), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((paged_attn_join_kernel<D, 1>), dim3(workgroups * (1 + kWide / kJoinRows)), dim3(256), 0, st, a);
     return hipGetLastError();
   }
   // More groups a row while that leaves at most about 1,024 workgroups.
@@ -1008,9 +1067,6 @@ hipError_t launch_paged(const PagedAttnArgs& a, hipStream_t st) {
 
 hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, int cu_count, hipStream_t st) {
   if (a.tokens == 0) return hipSuccess;
-  a.workgroups = workgroups_of(a.hkv, d, cu_count);
-  a.per_worker[kWideItem] = 1.0 / a.workgroups;
-  a.per_worker[kNarrowItem] = 0.25 / a.workgroups;
   a.item_cost[kNarrowItem] = 1;
   a.item_cost[kWideItem] = 2;
   a.min_chunk[kNarrowItem] = 2;
@@ -1020,6 +1076,16 @@ hipError_t launch_attn_paged(PagedAttnArgs a, int32_t d, int cu_count, hipStream
   if (const char* e = tuning_override("QM_PAGED_PLAN"))
     std::sscanf(e, "%d,%d,%d,%d,%d,%d", &a.item_cost[0], &a.item_cost[1], &a.min_chunk[0], &a.min_chunk[1], &a.min_part[0],
                 &a.min_part[1]);
+  // No more workgroups than the page tables leave work for.
+  const int64_t most_keys = static_cast<int64_t>(a.max_pages) << a.page_log2;
+  const int64_t narrow = std::min(a.n_req, a.tokens) * (a.item_cost[kNarrowItem] + (most_keys + 31) / 32) / a.min_chunk[kNarrowItem];
+  const int64_t wide = static_cast<int64_t>(a.tokens) * a.group <= kNarrow
+                           ? 0
+                           : 2 * (static_cast<int64_t>(a.tokens) * a.group / kWide + a.n_req + 1) *
+                                 (a.item_cost[kWideItem] + (most_keys + 63) / 64) / a.min_chunk[kWideItem];
+  a.workgroups = static_cast<int>(std::min<int64_t>(workgroups_of(a.hkv, d, cu_count), std::max((narrow + 3) / 4, wide) + 2));
+  a.per_worker[kWideItem] = 1.0 / a.workgroups;
+  a.per_worker[kNarrowItem] = 0.25 / a.workgroups;
   return d == 64 ? launch_paged<64>(a, st) : launch_paged<128>(a, st);
 }
 
