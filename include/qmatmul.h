@@ -508,7 +508,8 @@ qm_status qdec_argmax_rows(const float* logits, int64_t rows, int64_t n, int32_t
  * A prefix that all requests share (one system prompt) takes the first
  * prefix_pages entries of every page table; it is whole pages. */
 
-/* The bookkeeping of one step, in one launch.  Request i holds lens[i] tokens;
+/* The bookkeeping of one step, in one launch.  Request i holds lens[i] tokens
+ * (at least the prefix: 0 is a request that holds no more);
  * new_lens[i] >= 0 new ones come, or new_lens[i] < 0: the request has ended.
  * free_ring (int32 [n_pages]) is a ring of free page ids, ring = {head, count}:
  * entry j < count at (head + j) % n_pages.

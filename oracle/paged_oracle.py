@@ -20,6 +20,7 @@ def plan_step(lens, new_lens, tables, free_ring, ring, page, max_tokens, prefix_
     old = [list(t) for t in tables]
     for i, (length, new) in enumerate(zip(lens, new_lens)):
         sane = 0 <= length <= width * page
+        length = max(length, prefix_pages * page) if sane else length
         have = -(-length // page) if sane else 0
         if new < 0:
             if sane:

@@ -71,6 +71,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(KvPlanArgs a) {
   // t < 0: the request has ended.  More new tokens than the batch holds refuse
   // the request whatever their number, so the sums stay below 2^27.
   const bool sane = len >= 0 && len <= static_cast<int64_t>(a.max_pages) << a.page_log2;
+  if (sane) len = max(len, a.prefix_pages << a.page_log2);       // the prefix is there from the start
   const int add = i < n ? min(max(t, 0), a.max_tokens + 1) : 0;
   const int end = block_scan(add, sums[0]);
   const bool active = i < n && t >= 0;

@@ -1,4 +1,4 @@
-"""Host sequencing of one decode step of a dense grouped-query-attention
+"""Host sequencing of the decode steps of a dense grouped-query-attention
 decoder (the Llama 3.2 / Qwen3 layer) over the library's entry points
 (BaseRT Sec. 3.2: a token is embedding, per layer norm -> q/k/v projections
 -> RoPE and cache append -> attention -> output projection -> residual and
@@ -210,3 +210,128 @@ class DenseDecoder:
         B.qdec_rmsnorm(x[m - 1], self.norm, c.eps, residual=y[m - 1], out=self.h, stream=s)
         B.qmatmul_gemv(self.lm_head, self.h, out=self.logits, stream=s)
         B.qdec_argmax(self.logits, out=self.token, workspace=self.argmax_ws, stream=s)
+
+
+class BatchDecoder:
+    """Many requests decoded together over a paged KV cache: one step takes
+    any number of new tokens of every request (a prompt, a chunk of one, the
+    next token), through the prefill GEMMs, qkv_rope_append and
+    qattn_paged_f16, and leaves every request's next token.
+
+    Weights as for DenseDecoder.  n_req: requests at most (slots); n_pages:
+    pages of page_size tokens that they share; max_len: tokens of one request
+    at most (rounded up to pages); max_tokens: new tokens of one step at most,
+    all requests together.  Which request holds which pages, lengths and
+    positions live on the device (qkv_plan), so a step can be captured in a
+    HIP graph and replayed; the lengths go from one of two buffers to the
+    other, so an even number of steps has to be captured together."""
+
+    def __init__(self, cfg: DecoderConfig, emb: torch.Tensor, layers: List[LayerWeights], norm: torch.Tensor,
+                 lm_head: B.QWeight, n_req: int, n_pages: int, max_len: int, page_size: int = 64,
+                 max_tokens: int = 2048, rope_rows_interleaved: bool = False):
+        if rope_rows_interleaved and any(ly.q_norm is not None for ly in layers):
+            raise ValueError("per-head q/k norms need rows that are not interleaved")
+        self.cfg, self.emb, self.layers, self.norm, self.lm_head = cfg, emb, layers, norm, lm_head
+        self.n_req, self.page_size, self.max_tokens = n_req, page_size, max_tokens
+        self.interleaved = rope_rows_interleaved
+        max_pages = -(-max_len // page_size)
+        dev, c = emb.device, cfg
+        f32, f16, i32 = (dict(dtype=t, device=dev) for t in (torch.float32, torch.float16, torch.int32))
+        qd, kvd = c.n_q_heads * c.head_dim, c.n_kv_heads * c.head_dim
+        table_len = max_pages * page_size
+        self.rope_tab = (B.qdec_rope_table(table_len, c.head_dim, c.theta, device=dev) if c.rope_scaling is None else
+                         B.qdec_rope_table_llama3(table_len, c.head_dim, c.theta, c.rope_scaling, device=dev))
+        pool = (c.layers, n_pages, c.n_kv_heads, page_size, c.head_dim)
+        self.k_pages, self.v_pages = torch.zeros(pool, **f16), torch.zeros(pool, **f16)
+        self.tables = torch.full((n_req, max_pages), -1, **i32)
+        self.free_ring = torch.arange(n_pages, **i32)            # every page is free
+        self.prefix: Optional[torch.Tensor] = None               # page ids that all requests share
+        # Lengths and free ring before the next step: those of plans[turn ^ 1].
+        self.plans = [B.empty_kv_plan(n_req, 0, device=dev) for _ in range(2)]
+        self.turn = 0
+        for p in self.plans:
+            p.lens.zero_()
+            p.ring.copy_(torch.tensor([0, n_pages], **i32))
+        self._positions = torch.empty(max_tokens, **i32)
+        self._slots = torch.empty(max_tokens, dtype=torch.int64, device=dev)
+        self.x = torch.zeros((max_tokens, c.hidden), **f32)      # residual stream
+        # Normed input of a projection, behind a row of zeros: row offsets[i + 1] is request i's last token.
+        self.h = torch.zeros((1 + max_tokens, c.hidden), **f16)
+        self.q, self.k, self.v = (torch.zeros((max_tokens, n), **f32) for n in (qd, kvd, kvd))
+        self.q16 = torch.zeros((max_tokens, c.n_q_heads, c.head_dim), **f16)
+        self.o16 = torch.zeros((max_tokens, qd), **f16)
+        self.y_attn, self.y_ffn = (torch.zeros((max_tokens, c.hidden), **f32) for _ in range(2))
+        self.g16 = torch.zeros((max_tokens, c.inter), **f16)
+        self.last = torch.zeros((n_req, c.hidden), **f32)
+        self.last16 = torch.zeros((n_req, c.hidden), **f16)
+        self.logits = torch.zeros((n_req, c.vocab), **f32)
+        self.token = torch.zeros(n_req, **i32)                   # greedy next token of every request
+        self.ws = torch.empty(B.qattn_paged_workspace_bytes(c.n_q_heads, c.n_kv_heads, c.head_dim, n_req, max_tokens, 1),
+                              dtype=torch.uint8, device=dev)
+        self.ws_plain = torch.empty(B.qattn_paged_workspace_bytes(c.n_q_heads, c.n_kv_heads, c.head_dim, n_req,
+                                                                  max_tokens), dtype=torch.uint8, device=dev)
+        self.argmax_ws = torch.empty(B.qdec_argmax_rows_workspace_bytes(n_req), dtype=torch.uint8, device=dev)
+        self.scale = 1.0 / math.sqrt(c.head_dim)
+
+    @property
+    def plan(self) -> B.KvPlan:
+        """The last step's plan (lens, refused, offsets, ...)."""
+        return self.plans[self.turn ^ 1]
+
+    def step(self, tokens: torch.Tensor, new_lens: torch.Tensor, stream=None) -> None:
+        """tokens: int32 [T] on the device, T <= max_tokens, the requests' new
+        tokens one after the other in the order of the slots (places behind
+        the last one count nothing); new_lens: int32 [n_req], how many each
+        request has (0: none; -1: it has ended, its pages are free from the
+        next step on).  Leaves logits and the greedy next token of every
+        request with new tokens in self.logits[i] and self.token[i].  A request
+        that finds no pages is refused (self.plan.refused, kv_lens 0): its
+        tokens are not cached and its logits are of no use."""
+        c, s, t = self.cfg, stream, tokens.numel()
+        if not 1 <= t <= self.max_tokens:
+            raise ValueError(f"a step of {t} tokens: must be 1 .. max_tokens={self.max_tokens}")
+        before, own = self.plans[self.turn ^ 1], self.plans[self.turn]
+        plan = B.KvPlan(own.lens, own.kv_lens, own.offsets, self._positions[:t], self._slots[:t], own.ring, own.refused)
+        self.plans[self.turn] = plan
+        self.turn ^= 1
+        B.qkv_plan(before.lens, new_lens, self.tables, self.free_ring, before.ring, self.page_size, t,
+                   prefix_pages=0 if self.prefix is None else self.prefix.numel(), out=plan, stream=s)
+        x, h, y = self.x[:t], self.h[1:1 + t], None
+        ws = self.ws_plain if self.prefix is None else self.ws
+        B.qdec_embed_rows(self.emb, tokens, out=x, stream=s)
+        for li, ly in enumerate(self.layers):
+            B.qdec_rmsnorm(x, ly.attn_norm, c.eps, residual=y, out=h, stream=s)
+            q, k, v = B.qmatmul_gemm_grouped([ly.wq, ly.wk, ly.wv], h, outs=[self.q[:t], self.k[:t], self.v[:t]],
+                                             stream=s)
+            B.qkv_rope_append(q, k, v, plan.positions, plan.slots, self.rope_tab, self.k_pages[li], self.v_pages[li],
+                              interleaved=self.interleaved, q_norm=ly.q_norm, k_norm=ly.k_norm, eps=c.eps,
+                              q_out=self.q16[:t], stream=s)
+            B.qattn_paged_f16(self.q16[:t], self.k_pages[li], self.v_pages[li], self.tables, plan.offsets,
+                              plan.kv_lens, self.scale, prefix=self.prefix, out=self.o16[:t], workspace=ws, stream=s)
+            B.qmatmul_gemm(ly.wo, self.o16[:t], out=self.y_attn[:t], stream=s)
+            B.qdec_rmsnorm(x, ly.ffn_norm, c.eps, residual=self.y_attn[:t], out=h, stream=s)
+            B.qmatmul_gemm_swiglu_f16(ly.wg, ly.wu, h, out=self.g16[:t], stream=s)
+            y = B.qmatmul_gemm(ly.wd, self.g16[:t], out=self.y_ffn[:t], stream=s)
+        B.qdec_rmsnorm(x, self.norm, c.eps, residual=y, out=h, stream=s)
+        B.qdec_embed_rows(self.h[:1 + t], plan.offsets[1:], out=self.last, stream=s)
+        B.qdec_cast_f16(self.last, out=self.last16, stream=s)
+        B.qmatmul_gemm(self.lm_head, self.last16, out=self.logits, stream=s)
+        B.qdec_argmax_rows(self.logits, out=self.token, workspace=self.argmax_ws, stream=s)
+
+    def share_prefix(self, tokens: torch.Tensor, stream=None) -> None:
+        """Before any other step: runs tokens (int32 [n] on the device, n a
+        multiple of page_size) once and keeps them as the beginning of every
+        request."""
+        n = tokens.numel()
+        if self.prefix is not None or n == 0 or n % self.page_size or n > self.tables.shape[1] * self.page_size:
+            raise ValueError(f"a prefix of {n} tokens: one, of whole pages of {self.page_size}, within max_len")
+        new = torch.zeros(self.n_req, dtype=torch.int32, device=tokens.device)
+        for at in range(0, n, self.max_tokens):
+            part = tokens[at:at + self.max_tokens]
+            new[0] = part.numel()
+            self.step(part, new, stream=stream)
+        pages = n // self.page_size
+        if self.plan.refused.item():
+            raise RuntimeError(f"{pages} pages for the prefix are not there")
+        self.prefix = self.tables[0, :pages].clone()
+        self.tables[:, :pages] = self.prefix

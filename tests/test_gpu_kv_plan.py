@@ -87,6 +87,16 @@ def test_plan_gives_pages_back_around_the_ring():
     assert p.ring.tolist() == [6, 6]
 
 
+def test_plan_begins_behind_the_prefix():
+    """Lengths below the prefix count as the prefix, also where it fills the table."""
+    tables = [[8, 9, -1, -1], [8, 9, 3, 4], [8, 9, -1, -1], [8, 9, 2, -1], [8, 9, -1, -1]]
+    ring = [5, 6, 7] + [-1] * 7
+    for lens in ([0, 50, 0, 33, 0], [32, 31, 17, 48, 1]):
+        for new in ([3, -1, 0, 20, 33], [17, 1, -1, -1, 40], [0, 0, 0, 0, 0]):
+            _check(lens, new, tables, ring, [0, 3], 16, 64, prefix_pages=2)
+    _check([0, 10, 64], [0, 1, -1], tables[:3], ring, [0, 3], 16, 64, prefix_pages=4)
+
+
 def test_plan_is_the_same_when_repeated_and_in_replayed_graphs():
     """A captured plan follows the lengths: each replay takes the state that the
     program wrote in between, with eager work around it."""

@@ -29,6 +29,15 @@ def test_plan_refusals_by_hand():
     assert r["tables"] == [[0, 8], [1, -1], [2, -1], [3, 4]] and r["ring"] == [1, 0]
 
 
+def test_plan_with_a_prefix_by_hand():
+    # Two shared pages of 16: request 0 begins behind them, request 1 ends and keeps them, request 2 is idle.
+    r = PO.plan_step([0, 50, 0], [3, -1, 0], [[8, 9, -1, -1], [8, 9, 3, 4], [8, 9, -1, -1]], [5, -1, -1, -1], [0, 1], 16,
+                     4, prefix_pages=2)
+    assert r["tables"][0] == [8, 9, 5, -1] and r["positions"] == [32, 33, 34, -1] and r["slots"][:3] == [80, 81, 82]
+    assert r["lens"] == [35, 0, 32] and r["kv_lens"] == [35, 0, 32] and r["free_ring"] == [5, 3, 4, -1]
+    assert r["ring"] == [1, 2]
+
+
 def test_attention_equals_the_contiguous_oracle():
     rng = np.random.default_rng(0)
     hq, hkv, d, page, n, new = 4, 2, 64, 16, 37, 5
