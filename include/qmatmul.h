@@ -487,7 +487,7 @@ qm_status qdec_argmax(const float* logits, int64_t n, int32_t* token, void* work
  * (fp32 [rows][n], device), r < rows.  tokens: int32 [rows]; 0 <= rows <= 32768;
  * workspace: rows x QDEC_ARGMAX_WORKSPACE_BYTES (host-only query
  * qdec_argmax_rows_workspace_bytes), 4-byte aligned, contents not preserved.
- * One launch for n <= 4096, else two.
+ * One launch, two for few rows of many logits.
  * (Sec. 3.2: sampling kernel of the decode step, for several sequences.) */
 qm_status qdec_argmax_rows_workspace_bytes(int64_t rows, size_t* bytes);
 qm_status qdec_argmax_rows(const float* logits, int64_t rows, int64_t n, int32_t* tokens, void* workspace,

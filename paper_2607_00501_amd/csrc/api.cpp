@@ -782,7 +782,11 @@ qm_status qdec_argmax_rows(const float* logits, int64_t rows, int64_t n, int32_t
     return fail(QM_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", name, need, workspace ? ws_bytes : 0);
   if (!aligned4(logits) || !aligned4(tokens) || !aligned4(workspace))
     return fail(QM_EALIGN, "%s: logits, tokens and workspace 4-byte aligned", name);
-  return launched(launch_argmax(logits, rows, n, tokens, workspace, static_cast<hipStream_t>(stream)), name);
+  const DeviceInfo* d;
+  const qm_status st = device_info(&d);
+  if (st != QM_OK) return st;
+  return launched(launch_argmax_rows(logits, rows, n, tokens, workspace, d->cu_count, static_cast<hipStream_t>(stream)),
+                  name);
 }
 
 // Page size, as its logarithm, and page count of a paged cache.

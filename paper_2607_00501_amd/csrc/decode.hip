@@ -485,6 +485,53 @@ __global__ __launch_bounds__(256) void argmax_final_kernel(const float* __restri
   if (threadIdx.x == 0) token[blockIdx.y] = idx == INT32_MAX ? 0 : idx;
 }
 
+// A workgroup of 1,024 threads for a whole row: one launch.  The row begins with up
+// to three single logits, then 16-byte loads, eight of them on their way per thread.
+__global__ __launch_bounds__(1024) void argmax_row_kernel(const float* __restrict__ x, int64_t n,
+                                                          int32_t* __restrict__ token) {
+  constexpr int UN = 8;
+  __shared__ float sv[16];
+  __shared__ int32_t si[16];
+  x += blockIdx.x * n;
+  float best = -INFINITY;
+  int32_t idx = INT32_MAX;
+  auto see = [&](float v, int32_t i) __attribute__((always_inline)) {   // increasing i: the first of equal values
+    if (v > best || (v == best && idx == INT32_MAX)) {
+      best = v;
+      idx = i;
+    }
+  };
+  const int64_t head = min<int64_t>((0 - reinterpret_cast<uintptr_t>(x) / 4) & 3, n), n4 = (n - head) / 4;
+  if (static_cast<int64_t>(threadIdx.x) < head) see(x[threadIdx.x], threadIdx.x);
+  const float4* body = reinterpret_cast<const float4*>(x + head);
+  for (int64_t b = threadIdx.x; b < n4; b += 1024 * UN) {
+    float4 v[UN];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) v[u] = body[min(b + u * 1024, n4 - 1)];   // (past the end: the last ones again)
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int32_t i = static_cast<int32_t>(head + 4 * min(b + u * 1024, n4 - 1));
+      see(v[u].x, i);
+      see(v[u].y, i + 1);
+      see(v[u].z, i + 2);
+      see(v[u].w, i + 3);
+    }
+  }
+  for (int64_t i = head + 4 * n4 + threadIdx.x; i < n; i += 1024) see(x[i], static_cast<int32_t>(i));
+  for (int o = 32; o > 0; o >>= 1) take_better(best, idx, __shfl_xor(best, o, 64), __shfl_xor(idx, o, 64));
+  if ((threadIdx.x & 63) == 0) {
+    sv[threadIdx.x >> 6] = best;
+    si[threadIdx.x >> 6] = idx;
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    best = sv[threadIdx.x & 15];
+    idx = si[threadIdx.x & 15];
+    for (int o = 8; o > 0; o >>= 1) take_better(best, idx, __shfl_xor(best, o, 64), __shfl_xor(idx, o, 64));
+    if (threadIdx.x == 0) token[blockIdx.x] = idx == INT32_MAX ? 0 : idx;
+  }
+}
+
 unsigned spread_blocks(int64_t n) {
   const int64_t b = (n + 255) / 256;
   return static_cast<unsigned>(b < 1024 ? (b < 1 ? 1 : b) : 1024);
@@ -618,6 +665,16 @@ hipError_t launch_rope_append_paged(const KvAppendArgs& p, int32_t d, hipStream_
     hipLaunchKernelGGL(rope_append_paged_kernel<64>, grid, dim3(256), 0, st, p);
   else
     hipLaunchKernelGGL(rope_append_paged_kernel<128>, grid, dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+// A workgroup a row, or n / 4096 workgroups a row and a second launch where few rows
+// of many logits would leave most CUs idle (us, one launch / two: 5 rows of 32,001 5.8 /
+// 7.7, 3 of 65,536 8.4 / 6.5, 64 of 151,936 17.2 / 13.5, 200 of 151,936 24.8 / 29.2).
+hipError_t launch_argmax_rows(const float* x, int64_t rows, int64_t n, int32_t* token, void* ws, int cu_count,
+                              hipStream_t st) {
+  if (n > 49152 && 5 * rows < 2 * cu_count) return launch_argmax(x, rows, n, token, ws, st);
+  hipLaunchKernelGGL(argmax_row_kernel, dim3(static_cast<unsigned>(rows)), dim3(1024), 0, st, x, n, token);
   return hipGetLastError();
 }
 

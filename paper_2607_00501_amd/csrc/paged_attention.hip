@@ -31,6 +31,7 @@
 // made before it, and can be replayed from a graph while the lengths move on.
 #include "lds_dma.h"
 #include "qm_internal.h"
+#include "wave_scan.h"
 
 #include <algorithm>
 #include <cfloat>
@@ -82,18 +83,8 @@ __device__ __forceinline__ int request_of(const Requests& r, int n, int token) {
 }
 
 
-// Inclusive sum over the lanes of a wavefront.
-__device__ __forceinline__ int wave_scan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // row_shr:1, 2, 4, 8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast:15, 31
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
-  return v;
-}
-// The same for 0 <= v < 2^49, in two halves.
-__device__ __forceinline__ int64_t wave_scan(int64_t v) {
+// The inclusive sum over the lanes of 0 <= v < 2^49, in two halves.
+__device__ __forceinline__ int64_t wave_scan64(int64_t v) {
   const int lo = wave_scan(static_cast<int>(v & 0xFFFFFF)), hi = wave_scan(static_cast<int>(v >> 24));
   return (static_cast<int64_t>(hi) << 24) + lo;
 }
@@ -159,7 +150,7 @@ __device__ __forceinline__ Line make_line(const Requests& r, const PagedAttnArgs
     const Items t = items_of<K>(r, a, i);
     cost += t.cost(t.tiles);
   }
-  const int64_t upto = wave_scan(cost);
+  const int64_t upto = wave_scan64(cost);
   n.before = prefix + upto - cost;
   n.total = prefix + lane_value(upto, 63);
   n.chunk = max<int64_t>(static_cast<int64_t>(static_cast<double>(n.total) * a.per_worker[K]) + 1, a.min_chunk[K]);

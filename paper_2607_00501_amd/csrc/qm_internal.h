@@ -213,6 +213,8 @@ struct QkvRopeEpi {
 hipError_t launch_gemv_qkv_norm_rope(int32_t fmt, GemvGroup& g, const NormArgs& na, const QkvRopeEpi& epi,
                                      int64_t k, int cu_count, hipStream_t st);
 hipError_t launch_argmax(const float* x, int64_t rows, int64_t n, int32_t* token, void* ws, hipStream_t st);
+hipError_t launch_argmax_rows(const float* x, int64_t rows, int64_t n, int32_t* token, void* ws, int cu_count,
+                              hipStream_t st);
 
 // Batched serving over a paged KV cache: pools fp16 [n_pages][hkv][page][d].
 constexpr int64_t kArgmaxMaxRows = 32768;
