@@ -569,14 +569,18 @@ qm_status qkv_rope_append(const float* q, const float* k, const float* v, int32_
  * prefix_pages > 0: positions below prefix_pages * page_size are read from the
  * pages prefix[0 .. prefix_pages), once for all requests, and the tables'
  * entries for them are not read; the other keys as before.
+ * offsets rise from 0 to at most tokens, kv_lens are at most max_pages *
+ * page_size; others are held within these limits, and the rows of what then is
+ * no request may hold anything.
  * q: fp16 [tokens][n_q_heads][head_dim]; out: fp16 [tokens][n_q_heads *
- * head_dim] (the output projection's rows); rows past offsets[n_req] are left
- * as they were.  head_dim 64 or 128; n_kv_heads <= 128; n_q_heads <= 1024, a
- * multiple of it; 0 <= tokens <= 65536; scale finite and > 0.  A page id
- * outside [0, n_pages) among the keys that a 128-row tile of (token, head)
- * pairs sees makes that tile's rows NaN (no host synchronisation, so no status
- * code).  Scores, maxima and sums in fp32; the weights go to the MFMA in fp16
- * (to nearest).  Two launches.  Deterministic.
+ * head_dim] (the output projection's rows), not q; rows past offsets[n_req] are
+ * left as they were.  head_dim 64 or 128; n_kv_heads <= 128; n_q_heads <= 1024,
+ * a multiple of it, at most 128 times; 0 <= tokens <= 65536; scale finite and
+ * > 0.  A page id outside [0, n_pages) among the keys of a request (or of the
+ * prefix) makes rows that see them, up to 128 (token, head) pairs at a time,
+ * NaN (no host synchronisation, so no status code).  Scores, maxima and sums in
+ * fp32; the weights go to the MFMA in fp16 (to nearest).  Two launches.
+ * Deterministic.
  * q, pools, out and workspace 16-byte aligned; workspace of at least
  * qattn_paged_workspace_bytes for this n_req, tokens and prefix_pages (device
  * scratch, contents not preserved; calls that share it must not overlap). */

@@ -918,6 +918,7 @@ qm_status qattn_paged_f16(const uint16_t* q, const uint16_t* k_pages, const uint
     return fail(QM_EALIGN, "%s: q, pools, out and workspace must be 16-byte aligned", name);
   if (!aligned4(tables) || !aligned4(prefix) || !aligned4(offsets) || !aligned4(kv_lens))
     return fail(QM_EALIGN, "%s: tables, prefix, offsets and kv_lens must be 4-byte aligned", name);
+  if (out == q) return fail(QM_EINVAL, "%s: out must not be q (several workgroups read a row)", name);
   const DeviceInfo* d;
   if ((st = device_info(&d)) != QM_OK) return st;
   const size_t need =

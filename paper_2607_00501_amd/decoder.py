@@ -290,15 +290,17 @@ class BatchDecoder:
         c, s, t = self.cfg, stream, tokens.numel()
         if not 1 <= t <= self.max_tokens:
             raise ValueError(f"a step of {t} tokens: must be 1 .. max_tokens={self.max_tokens}")
-        before, own = self.plans[self.turn ^ 1], self.plans[self.turn]
-        plan = B.KvPlan(own.lens, own.kv_lens, own.offsets, self._positions[:t], self._slots[:t], own.ring, own.refused)
-        self.plans[self.turn] = plan
-        self.turn ^= 1
-        B.qkv_plan(before.lens, new_lens, self.tables, self.free_ring, before.ring, self.page_size, t,
-                   prefix_pages=0 if self.prefix is None else self.prefix.numel(), out=plan, stream=s)
+        if tokens.dtype != torch.int32 or tokens.device != self.emb.device or not tokens.is_contiguous():
+            raise ValueError(f"tokens: need contiguous int32 on {self.emb.device}, got {tokens.dtype} on {tokens.device}")
         x, h, y = self.x[:t], self.h[1:1 + t], None
         ws = self.ws_plain if self.prefix is None else self.ws
         B.qdec_embed_rows(self.emb, tokens, out=x, stream=s)
+        before, own = self.plans[self.turn ^ 1], self.plans[self.turn]
+        plan = B.KvPlan(own.lens, own.kv_lens, own.offsets, self._positions[:t], self._slots[:t], own.ring, own.refused)
+        B.qkv_plan(before.lens, new_lens, self.tables, self.free_ring, before.ring, self.page_size, t,
+                   prefix_pages=0 if self.prefix is None else self.prefix.numel(), out=plan, stream=s)
+        self.plans[self.turn] = plan                             # (a refused call leaves everything as it was)
+        self.turn ^= 1
         for li, ly in enumerate(self.layers):
             B.qdec_rmsnorm(x, ly.attn_norm, c.eps, residual=y, out=h, stream=s)
             q, k, v = B.qmatmul_gemm_grouped([ly.wq, ly.wk, ly.wv], h, outs=[self.q[:t], self.k[:t], self.v[:t]],
@@ -321,17 +323,18 @@ class BatchDecoder:
     def share_prefix(self, tokens: torch.Tensor, stream=None) -> None:
         """Before any other step: runs tokens (int32 [n] on the device, n a
         multiple of page_size) once and keeps them as the beginning of every
-        request."""
-        n = tokens.numel()
+        request.  Waits for the device."""
+        n, pages = tokens.numel(), tokens.numel() // self.page_size
         if self.prefix is not None or n == 0 or n % self.page_size or n > self.tables.shape[1] * self.page_size:
             raise ValueError(f"a prefix of {n} tokens: one, of whole pages of {self.page_size}, within max_len")
-        new = torch.zeros(self.n_req, dtype=torch.int32, device=tokens.device)
-        for at in range(0, n, self.max_tokens):
-            part = tokens[at:at + self.max_tokens]
-            new[0] = part.numel()
-            self.step(part, new, stream=stream)
-        pages = n // self.page_size
-        if self.plan.refused.item():
-            raise RuntimeError(f"{pages} pages for the prefix are not there")
-        self.prefix = self.tables[0, :pages].clone()
-        self.tables[:, :pages] = self.prefix
+        with torch.cuda.stream(stream):
+            if self.plan.lens.any().item() or self.plan.ring[1].item() < pages:
+                raise ValueError(f"a prefix comes before any other step and has to find its {pages} pages")
+            for at in range(0, n, self.max_tokens):
+                part = tokens[at:at + self.max_tokens]
+                new = torch.zeros(self.n_req, dtype=torch.int32, device=tokens.device)
+                new[0] = part.numel()
+                self.step(part, new, stream=stream)
+            self.prefix = self.tables[0, :pages].clone()
+            self.tables[:, :pages] = self.prefix
+            torch.cuda.current_stream().synchronize()

@@ -137,3 +137,44 @@ def test_replayed_steps_equal_eager_ones():
         torch.cuda.synchronize()
         assert torch.equal(decs[0].logits, decs[1].logits) and torch.equal(decs[0].token, decs[1].token)
         assert torch.equal(decs[0].plan.lens, decs[1].plan.lens)
+
+
+def test_refused_steps_and_prefixes_change_nothing():
+    """Wrong arguments, a prefix after a step, one whose pages are not there (its last
+    part alone would find some): as if they had not been made."""
+    layers, emb, norm, head, ref = _model(TINY, 64)
+    dec = BatchDecoder(TINY, emb, layers, norm, head, n_req=2, n_pages=7, max_len=256, page_size=16, max_tokens=48)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        dec.share_prefix(torch.zeros(128, **i32))                    # 8 pages, parts of 3, 3 and 2
+    _step(dec, {0: [5, 6, 7], 1: [8]})
+    want = _Oracle(ref, TINY, 256)
+    want.feed([5, 6, 7])
+    for tokens, new in [(torch.zeros(2, **i32), torch.ones(3, **i32)),
+                        (torch.zeros(2, **i32), torch.ones(2, dtype=torch.int64, device="cuda")),
+                        (torch.zeros(2, **i32), torch.ones(2, dtype=torch.int32)),
+                        (torch.zeros(2, dtype=torch.int32), torch.ones(2, **i32))]:
+        with pytest.raises(ValueError):
+            dec.step(tokens, new)
+    with pytest.raises(ValueError):
+        dec.share_prefix(torch.zeros(16, **i32))
+    _step(dec, {0: [9]})
+    assert dec.plan.lens.tolist() == [4, 1] and dec.plan.ring.tolist() == [2, 5]
+    assert rel_err(dec.logits[0].cpu().numpy(), want.feed([9])) <= MFMA_TOL
+
+
+def test_steps_on_another_stream():
+    """A prefix in parts and steps, all on a stream of their own."""
+    layers, emb, norm, head, _ = _model(TINY, 65)
+    tokens = torch.arange(7, 7 + 96, dtype=torch.int32, device="cuda")
+    new = torch.tensor([3, 0, 2], dtype=torch.int32, device="cuda")
+    logits = []
+    for stream in (None, torch.cuda.Stream()):
+        dec = BatchDecoder(TINY, emb, layers, norm, head, n_req=3, n_pages=20, max_len=256, page_size=16, max_tokens=40)
+        torch.cuda.synchronize()
+        dec.share_prefix(tokens, stream=stream)
+        dec.step(tokens[:5], new, stream=stream)
+        torch.cuda.synchronize()
+        assert dec.plan.lens.tolist() == [99, 96, 98]                # (all hold the prefix)
+        logits.append(dec.logits[[0, 2]].clone())
+    assert torch.equal(*logits)

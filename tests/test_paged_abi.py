@@ -59,7 +59,7 @@ def test_append_refusals(change, status):
 
 
 ATTEND = dict(q=P, k_pages=P, v_pages=P, n_pages=10, page_size=16, tables=P, max_pages=4, prefix=P, prefix_pages=1,
-              offsets=P, kv_lens=P, n_req=2, tokens=2, hq=4, hkv=2, d=64, scale=0.1, out=P, workspace=P,
+              offsets=P, kv_lens=P, n_req=2, tokens=2, hq=4, hkv=2, d=64, scale=0.1, out=ctypes.c_void_p(0x60000), workspace=P,
               ws_bytes=1 << 40, stream=None)
 
 
@@ -68,7 +68,7 @@ ATTEND = dict(q=P, k_pages=P, v_pages=P, n_pages=10, page_size=16, tables=P, max
     (dict(max_pages=0), ESHAPE), (dict(prefix_pages=5), ESHAPE), (dict(prefix_pages=-1), ESHAPE),
     (dict(n_req=0), ESHAPE), (dict(n_req=2000), ESHAPE), (dict(tokens=-1), ESHAPE), (dict(tokens=65537), ESHAPE),
     (dict(hq=3), ESHAPE), (dict(hq=0), ESHAPE), (dict(hkv=0), ESHAPE), (dict(hq=129, hkv=129), ESHAPE),
-    (dict(hq=1026), ESHAPE), (dict(d=96), ESHAPE), (dict(scale=0.0), EINVAL), (dict(scale=-1.0), EINVAL),
+    (dict(hq=1026), ESHAPE), (dict(hq=258), ESHAPE), (dict(out=P), EINVAL), (dict(d=96), ESHAPE), (dict(scale=0.0), EINVAL), (dict(scale=-1.0), EINVAL),
     (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL),
     *[({k: None}, EINVAL) for k in ("q", "k_pages", "v_pages", "tables", "prefix", "offsets", "kv_lens", "out")],
     *[({k: FOUR}, EALIGN) for k in ("q", "k_pages", "v_pages", "out", "workspace")],
@@ -88,6 +88,18 @@ def test_row_argmax_refusals():
     assert B.qdec_argmax_rows_workspace_bytes(0) == 0
     with pytest.raises(B.QmError):
         B.qdec_argmax_rows_workspace_bytes(-1)
+
+
+def test_batch_decoder_leaves_its_state_at_a_refusal():
+    """Tokens of a wrong type or place are refused before anything is counted."""
+    from paper_2607_00501_amd.decoder import BatchDecoder
+    dec = BatchDecoder.__new__(BatchDecoder)
+    dec.max_tokens, dec.emb, dec.turn, dec.cfg = 8, torch.zeros(4, 4), 0, None
+    for tokens in (torch.zeros(9, dtype=torch.int32), torch.zeros(0, dtype=torch.int32), torch.zeros(3),
+                   torch.zeros((8, 2), dtype=torch.int32)[:, 0], torch.zeros(3, dtype=torch.int32, device="meta")):
+        with pytest.raises(ValueError):
+            dec.step(tokens, None)
+        assert dec.turn == 0
 
 
 def test_nothing_to_do_is_no_error():
