@@ -505,6 +505,7 @@ template <int D>
 __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s, const uint16_t* q_row, int limit,
                                           int head, const Keys& k, float16v (&acc)[D / 32], float& m, float& l) {
   constexpr int KS = D / 16, DB = D / 32, C = D / 8, PIECES = D / 32;   // PIECES: KiB of 16 keys
+  constexpr int AHEAD = D == 64 ? 6 : 8;                                // fragments of V read before the softmax
   const int thread = fresh_thread(), lane = thread & 63, col = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int page_rows = 1 << a.page_log2, hi = k.hi;
@@ -560,7 +561,7 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
       qg::lds_dma16(a.v_pages + row * D, v_off[j], &s.v[buf][16 * wave * D + 512 * j]);
     }
   };
-  auto compute = [&](int buf, int kb) __attribute__((always_inline)) {
+  auto compute = [&]<bool MASKED>(int buf, int kb) __attribute__((always_inline)) {
     const _Float16* const kl = s.k[buf];
     const _Float16* const vl = s.v[buf];
     float16v st[2];
@@ -568,25 +569,39 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) st[t][r] = 0.0f;
+    // Fragments in groups of eight, read ahead of their use (left to itself the compiler
+    // reads one, waits for it and multiplies).
+    auto key_at = [&](int c, int t) __attribute__((always_inline)) {
+      return *reinterpret_cast<const half8v*>(&kl[(32 * t + col) * D + (((2 * c + lh) ^ k_swizzle<D>(col)) << 3)]);
+    };
+    half8v kf[2 * KS];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) kf[x] = key_at(x / 2, x & 1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int c = 0; c < KS; ++c)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const half8v f =
-            *reinterpret_cast<const half8v*>(&kl[(32 * t + col) * D + (((2 * c + lh) ^ k_swizzle<D>(col)) << 3)]);
-        st[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, qf[c], st[t], 0, 0, 0);
+        st[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[2 * c + t], qf[c], st[t], 0, 0, 0);
+        if (c + 4 < KS) kf[2 * c + 8 + t] = key_at(c + 4, t);
+        if (c + 4 < KS) __builtin_amdgcn_sched_barrier(0);
       }
-    // Fragments a few MFMAs ahead of their use.
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    // k slot (lh, j) of step kk: key 16 kk + 8 (j / 4) + 4 lh + j % 4.
+    auto value = [&](int kk, int b) __attribute__((always_inline)) {
+      const int row = 16 * kk + 4 * lh + ((lane & 15) >> 2), dim = 32 * b + (col & 16) + 4 * (lane & 3);
+      const half4v lo = read_tr(&vl[v_at<D>(row, dim)]);
+      const half4v up = read_tr(&vl[v_at<D>(row + 8, dim)]);
+      return half8v{lo[0], lo[1], lo[2], lo[3], up[0], up[1], up[2], up[3]};
+    };
+    half8v vf[4 * DB];
+    if constexpr (!MASKED) {
 #pragma unroll
-    for (int c = 0; c < 2 * KS - 4; ++c) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      for (int x = 0; x < AHEAD; ++x) vf[x] = value(x / DB, x % DB);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     // Lane: row col, keys kb + 32 t + 8 (r / 4) + 4 lh + r % 4.
-    const bool masked = kb + kBlock > all;
-    if (masked) {
+    if constexpr (MASKED) {
       const int seen = min(limit, hi) - kb - 4 * lh;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -621,26 +636,14 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
         x[(r & 7) + 1] = static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(st[t][r + 1], a.scale_log2, shift)));
         l = add_pair(x, r & 7, l);
       }
-    // k slot (lh, j) of step kk: key 16 kk + 8 (j / 4) + 4 lh + j % 4.
-    auto value = [&](int kk, int b) __attribute__((always_inline)) {
-      const int row = 16 * kk + 4 * lh + ((lane & 15) >> 2), dim = 32 * b + (col & 16) + 4 * (lane & 3);
-      const half4v lo = read_tr(&vl[v_at<D>(row, dim)]);
-      const half4v up = read_tr(&vl[v_at<D>(row + 8, dim)]);
-      return half8v{lo[0], lo[1], lo[2], lo[3], up[0], up[1], up[2], up[3]};
-    };
-    if (!masked) {
+    if constexpr (!MASKED) {
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
+      for (int x = AHEAD; x < 4 * DB; ++x) vf[x] = value(x / DB, x % DB);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int b = 0; b < DB; ++b)
-          acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(kk, b), w[kk], acc[b], 0, 0, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
-#pragma unroll
-      for (int c = 0; c < 4 * DB - 4; ++c) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
+      for (int x = 0; x < 4 * DB; ++x)
+        acc[x % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[x], w[x / DB], acc[x % DB], 0, 0, 0);
     } else {                                                // as in narrow_part
       bool odd = false;
 #pragma unroll
@@ -663,19 +666,26 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
       }
     }
   };
+  // A block that this wavefront has copied is there and its reads of the other one are
+  // done; after the barrier so are everybody's.
+  auto step = [&](int buf, int kb) __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);                     // lgkmcnt(0)
+    qg::vm_wait<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (kb + kBlock < hi) copy(buf ^ 1, kb + kBlock);
+  };
   if (k.lo < hi) {
     copy(0, k.lo);
-    int buf = 0;
-    for (int kb = k.lo; kb < hi; kb += kBlock, buf ^= 1) {
-      // This wavefront's copies have landed and its reads of the other block are
-      // done; after the barrier so are everybody's.
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_waitcnt(0xC07F);                   // lgkmcnt(0)
-      qg::vm_wait<0>();
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      if (kb + kBlock < hi) copy(buf ^ 1, kb + kBlock);
-      if (kb < most) compute(buf, kb);
+    int buf = 0, kb = k.lo;
+    for (; kb + kBlock <= all; kb += kBlock, buf ^= 1) {
+      step(buf, kb);
+      compute.template operator()<false>(buf, kb);
+    }
+    for (; kb < hi; kb += kBlock, buf ^= 1) {
+      step(buf, kb);
+      if (kb < most) compute.template operator()<true>(buf, kb);
     }
   }
   __syncthreads();
