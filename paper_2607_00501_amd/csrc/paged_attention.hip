@@ -575,18 +575,29 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
       return *reinterpret_cast<const half8v*>(&kl[(32 * t + col) * D + (((2 * c + lh) ^ k_swizzle<D>(col)) << 3)]);
     };
     half8v kf[2 * KS];
+    float bm = -INFINITY;
 #pragma unroll
-    for (int x = 0; x < 8; ++x) kf[x] = key_at(x / 2, x & 1);
+    for (int x = 0; x < 8; ++x) kf[x] = key_at(x % KS, x / KS);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int c = 0; c < KS; ++c)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        st[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[2 * c + t], qf[c], st[t], 0, 0, 0);
-        if (c + 4 < KS) kf[2 * c + 8 + t] = key_at(c + 4, t);
-        if (c + 4 < KS) __builtin_amdgcn_sched_barrier(0);
+    for (int c = 0; c < KS; ++c) {
+      st[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[c], qf[c], st[0], 0, 0, 0);
+      if (KS > 4) {
+        kf[KS + c] = key_at(c, 1);
+        __builtin_amdgcn_sched_barrier(0);
       }
-    __builtin_amdgcn_sched_barrier(0);
+    }
+    // (the first keys' maxima while the second ones' products are on their way)
+#pragma unroll
+    for (int c = 0; c < KS; ++c) {
+      st[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[KS + c], qf[c], st[1], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!MASKED) {
+#pragma unroll
+        for (int r = c * 16 / KS; r < (c + 1) * 16 / KS; ++r) bm = fmaxf(bm, st[0][r]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
     // k slot (lh, j) of step kk: key 16 kk + 8 (j / 4) + 4 lh + j % 4.
     auto value = [&](int kk, int b) __attribute__((always_inline)) {
       const int row = 16 * kk + 4 * lh + ((lane & 15) >> 2), dim = 32 * b + (col & 16) + 4 * (lane & 3);
@@ -608,9 +619,8 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
 #pragma unroll
         for (int r = 0; r < 16; ++r) st[t][r] = 32 * t + 8 * (r >> 2) + (r & 3) < seen ? st[t][r] : -INFINITY;
     }
-    float bm = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = MASKED ? 0 : 1; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) bm = fmaxf(bm, st[t][r]);
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(bm), __float_as_uint(bm), false, false);
@@ -627,24 +637,37 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
     }
     const float shift = kWeightBits - m;
     half8v w[4];
+    auto weights = [&](int p) __attribute__((always_inline)) {   // pair p of 16
+      const int t = p / 8, r = 2 * (p % 8);
+      half8v& x = w[2 * t + (r >> 3)];
+      x[r & 7] = static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(st[t][r], a.scale_log2, shift)));
+      x[(r & 7) + 1] = static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(st[t][r + 1], a.scale_log2, shift)));
+      l = add_pair(x, r & 7, l);
+    };
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        half8v& x = w[2 * t + (r >> 3)];
-        x[r & 7] = static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(st[t][r], a.scale_log2, shift)));
-        x[(r & 7) + 1] = static_cast<_Float16>(__builtin_amdgcn_exp2f(fmaf(st[t][r + 1], a.scale_log2, shift)));
-        l = add_pair(x, r & 7, l);
-      }
+    for (int p = 0; p < 8; ++p) weights(p);
     if constexpr (!MASKED) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int x = AHEAD; x < 4 * DB; ++x) vf[x] = value(x / DB, x % DB);
       __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int x = 0; x < 4 * DB; ++x)
+      auto product = [&](int x) __attribute__((always_inline)) {
         acc[x % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[x], w[x / DB], acc[x % DB], 0, 0, 0);
+      };
+      // (the second keys' weights between the first ones' products)
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+#pragma unroll
+        for (int x = p * DB / 2; x < (p + 1) * DB / 2; ++x) product(x);
+        weights(8 + 2 * p);
+        weights(9 + 2 * p);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int x = 2 * DB; x < 4 * DB; ++x) product(x);
     } else {                                                // as in narrow_part
+#pragma unroll
+      for (int p = 8; p < 16; ++p) weights(p);
       bool odd = false;
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
