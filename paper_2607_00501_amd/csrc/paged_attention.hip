@@ -315,16 +315,18 @@ __device__ __forceinline__ half4v read_tr(const _Float16* p) {
 }
 
 // K and V in LDS: rows of D halves, the 16-byte chunk c of row r at chunk
-// c ^ swizzle(r).  K is read as 16 bytes of 32 rows at once: eight lanes, on rows
-// one after the other, fall on different banks.  V is read transposed, four rows x
-// 32 bytes by 16 lanes: they do with twice the row.
+// c ^ swizzle(r), so that the 256 bytes that are read at once fall on different banks:
+// of K 16 bytes of 16 rows one after the other; of V, transposed, 32 bytes of eight rows
+// (narrow tiles) or 64 bytes of four (wide ones).
 template <int D>
-__device__ __forceinline__ constexpr int k_swizzle(int row) { return row & (D / 8 - 1); }
-template <int D>
-__device__ __forceinline__ constexpr int v_swizzle(int row) { return (2 * row) & (D / 8 - 1); }
-template <int D>
+__device__ __forceinline__ constexpr int k_swizzle(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
+template <int D, Kind K>
+__device__ __forceinline__ constexpr int v_swizzle(int row) {
+  return K == kWideItem ? (D == 64 ? 2 * row & 7 : 4 * row & 15) : (D == 64 ? row & 6 : 2 * row & 15);
+}
+template <int D, Kind K>
 __device__ __forceinline__ int v_at(int row, int dim) {
-  return row * D + (((dim >> 3) ^ v_swizzle<D>(row)) << 3) + (dim & 7);
+  return row * D + (((dim >> 3) ^ v_swizzle<D, K>(row)) << 3) + (dim & 7);
 }
 
 constexpr int kBlock = kKeys<kWideItem>;
@@ -418,7 +420,7 @@ __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, _Float16* vl
 #pragma unroll
     for (int j = 0; j < VL; ++j) {
       const int piece = lane + 64 * j;
-      *reinterpret_cast<half8v*>(&vl[v_at<D>(piece / (D / 8), piece % (D / 8) * 8)]) = x.v[j];
+      *reinterpret_cast<half8v*>(&vl[v_at<D, kNarrowItem>(piece / (D / 8), piece % (D / 8) * 8)]) = x.v[j];
     }
     float4v st[2];
 #pragma unroll
@@ -463,8 +465,8 @@ __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, _Float16* vl
     }
     // k slot (g, j) of the second product: key 16 (j / 4) + 4 g + j % 4.
     auto value = [&](int b) __attribute__((always_inline)) {
-      const half4v lo = read_tr(&vl[v_at<D>(4 * g + (col >> 2), 16 * b + 4 * (col & 3))]);
-      const half4v up = read_tr(&vl[v_at<D>(16 + 4 * g + (col >> 2), 16 * b + 4 * (col & 3))]);
+      const half4v lo = read_tr(&vl[v_at<D, kNarrowItem>(4 * g + (col >> 2), 16 * b + 4 * (col & 3))]);
+      const half4v up = read_tr(&vl[v_at<D, kNarrowItem>(16 + 4 * g + (col >> 2), 16 * b + 4 * (col & 3))]);
       return half8v{lo[0], lo[1], lo[2], lo[3], up[0], up[1], up[2], up[3]};
     };
     if (!masked) {
@@ -485,7 +487,7 @@ __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, _Float16* vl
             for (int b = 0; b < DB; ++b)
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                const float x = static_cast<float>(vl[v_at<D>(key, 16 * b + 4 * g + r)]);
+                const float x = static_cast<float>(vl[v_at<D, kNarrowItem>(key, 16 * b + 4 * g + r)]);
                 acc[b][r] += __builtin_fabsf(x) < INFINITY ? 0.0f : x;
               }
           }
@@ -556,7 +558,7 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
   for (int j = 0; j < PIECES; ++j) {
     const int r = j * (64 / C) + lane / C;
     k_off[j] = 2 * (r * D + (((lane % C) ^ k_swizzle<D>(r)) << 3));
-    v_off[j] = 2 * (r * D + (((lane % C) ^ v_swizzle<D>(r)) << 3));
+    v_off[j] = 2 * (r * D + (((lane % C) ^ v_swizzle<D, kWideItem>(r)) << 3));
   }
   auto copy = [&](int buf, int kb) __attribute__((always_inline)) {
     const int n = (kb - k.lo) / kBlock & 63;
@@ -610,8 +612,8 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
     // k slot (lh, j) of step kk: key 16 kk + 8 (j / 4) + 4 lh + j % 4.
     auto value = [&](int kk, int b) __attribute__((always_inline)) {
       const int row = 16 * kk + 4 * lh + ((lane & 15) >> 2), dim = 32 * b + (col & 16) + 4 * (lane & 3);
-      const half4v lo = read_tr(&vl[v_at<D>(row, dim)]);
-      const half4v up = read_tr(&vl[v_at<D>(row + 8, dim)]);
+      const half4v lo = read_tr(&vl[v_at<D, kWideItem>(row, dim)]);
+      const half4v up = read_tr(&vl[v_at<D, kWideItem>(row + 8, dim)]);
       return half8v{lo[0], lo[1], lo[2], lo[3], up[0], up[1], up[2], up[3]};
     };
     half8v vf[4 * DB];
@@ -690,7 +692,7 @@ __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s,
             for (int b = 0; b < DB; ++b)
 #pragma unroll
               for (int r = 0; r < 16; ++r) {
-                const float x = static_cast<float>(vl[v_at<D>(key, 32 * b + 8 * (r >> 2) + 4 * lh + (r & 3))]);
+                const float x = static_cast<float>(vl[v_at<D, kWideItem>(key, 32 * b + 8 * (r >> 2) + 4 * lh + (r & 3))]);
                 acc[b][r] += __builtin_fabsf(x) < INFINITY ? 0.0f : x;
               }
           }
