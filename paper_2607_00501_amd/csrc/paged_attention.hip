@@ -18,7 +18,7 @@
 //   prefix items:  a tile of rows of any requests  x  the prefix keys,
 //   own items:     a tile of one request's rows    x  its own keys.
 // Items of more than 16 rows are the work of a workgroup (128 rows, 32 per
-// wavefront, keys shared through LDS), bound by the MFMA; the others, a single
+// wavefront, keys shared through LDS), bound by MFMA and softmax; the others, a single
 // token's group of heads, of a wavefront by itself, bound by HBM.  The items of
 // each kind and KV head, laid end to end and each as long as it costs, are cut into
 // equal lengths, one for each workgroup (or wavefront) that the CUs hold at once:
@@ -508,9 +508,12 @@ __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, _Float16* vl
 // limit: keys visible to this lane's row (lane & 31).  acc[b][r]: dimension
 // 32 b + 8 (r / 4) + 4 (lane / 32) + r % 4 of the row; m, l: its maximum and this
 // lane's share of the sum of weights.  Per block a wavefront takes 512 cycles of MFMA and
-// 790 of VALU with heads of 64, 1,024 and 950 with heads of 128, mostly in turn: a prompt
-// of 1,024 tokens after 16,384 at 748 and 868 TFLOP/s, 1,000 tokens after 16,384
-// shared ones at 751 (24 / 8 heads of 128).
+// 860 of VALU with heads of 64, 1,024 and 990 with heads of 128, which overlap between
+// wavefronts in part: a prompt of 1,024 tokens after 16,384 at 752 and 884 TFLOP/s (32 / 8
+// heads), 1,000 tokens after 16,384 shared ones at 734 (24 / 8 heads of 128).
+// Blocks that every row sees have a loop of their own: with a branch for the others in
+// it the compiler copied all sums twice a block (that and the reads of fragments eight
+// at a time: 345 -> 326 us for this prompt with heads of 128).
 template <int D>
 __device__ __forceinline__ void wide_part(const PagedAttnArgs& a, WideLds<D>& s, const uint16_t* q_row, int limit,
                                           int head, const Keys& k, float16v (&acc)[D / 32], float& m, float& l) {
