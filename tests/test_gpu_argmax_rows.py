@@ -38,3 +38,18 @@ def test_rows_past_32_bits():
     x[-1, 262146], x[0, 5], x[16390, 70000] = 1, 1, 1
     got = B.qdec_argmax_rows(x)
     assert got[-1].item() == 262146 and got[0].item() == 5 and got[16390].item() == 70000 and got[1].item() == 0
+
+
+@pytest.mark.parametrize("rows", [1, 102, 103])
+@pytest.mark.parametrize("n", [49152, 49153, 60001])
+def test_both_ways_at_their_border(rows, n):
+    """Rows that begin at every place of 16 bytes, ties, NaNs and infinities at the ends."""
+    g = torch.Generator(device="cuda").manual_seed(n + rows)
+    inf, nan = float("inf"), float("nan")
+    for shift in range(4):
+        x = torch.randint(-900, 900, (rows * n + shift,), generator=g, device="cuda").float()[shift:].view(rows, n)
+        x[0, :], x[0, n - 1], x[-1, 0] = nan, -inf, inf
+        got = B.qdec_argmax_rows(x)
+        clean = torch.where(x.isnan(), -inf, x)
+        best = (clean == clean.amax(1, keepdim=True)) & ~x.isnan()
+        assert torch.equal(got.long(), torch.where(best, torch.arange(n, device="cuda"), n).amin(1))
