@@ -1,7 +1,8 @@
 """MI355X (gfx950) weight-only-quantised matmul: Q4/Q8 group-32 fused
-dequantise+GEMV, Q4 MFMA GEMM and a top-k-routed MoE expert layer, behind
-the C ABI in include/qmatmul.h (libqmatmul.so).  ``binding`` holds the thin
-ctypes layer; ``inputs`` the seeded synthetic input generators; ``workloads``
+dequantise+GEMV, Q4 MFMA GEMM and a top-k-routed MoE expert layer, attention
+over contiguous and paged KV caches, behind the C ABI in include/qmatmul.h
+(libqmatmul.so).  ``binding`` holds the thin ctypes layer; ``decoder`` whole
+decode steps of one request or of a batch; ``inputs`` the seeded synthetic input generators; ``workloads``
 the layer shapes of the benchmark workloads."""
 
 from . import binding, inputs, workloads  # noqa: F401
