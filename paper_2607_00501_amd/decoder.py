@@ -11,7 +11,7 @@ the sampled token stays on the device for the next step's embedding.
 """
 
 import math
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 from typing import List, Optional
 
 import torch
@@ -222,9 +222,9 @@ class BatchDecoder:
     pages of page_size tokens that they share; max_len: tokens of one request
     at most (rounded up to pages); max_tokens: new tokens of one step at most,
     all requests together.  Which request holds which pages, lengths and
-    positions live on the device (qkv_plan), so a step can be captured in a
-    HIP graph and replayed; the lengths go from one of two buffers to the
-    other, so an even number of steps has to be captured together."""
+    positions live on the device (qkv_plan), and a step leaves them where it
+    found them, so a step (or several) can be captured in a HIP graph and
+    replayed between eager steps in any order."""
 
     def __init__(self, cfg: DecoderConfig, emb: torch.Tensor, layers: List[LayerWeights], norm: torch.Tensor,
                  lm_head: B.QWeight, n_req: int, n_pages: int, max_len: int, page_size: int = 64,
@@ -246,12 +246,13 @@ class BatchDecoder:
         self.tables = torch.full((n_req, max_pages), -1, **i32)
         self.free_ring = torch.arange(n_pages, **i32)            # every page is free
         self.prefix: Optional[torch.Tensor] = None               # page ids that all requests share
-        # Lengths and free ring before the next step: those of plans[turn ^ 1].
-        self.plans = [B.empty_kv_plan(n_req, 0, device=dev) for _ in range(2)]
-        self.turn = 0
-        for p in self.plans:
-            p.lens.zero_()
-            p.ring.copy_(torch.tensor([0, n_pages], **i32))
+        # Lengths, and the free ring's head and count, before a step and behind it: qkv_plan writes other
+        # places than it reads, and the step brings its result back to where the next one looks.
+        self._before, self._behind = (torch.zeros(n_req + 2, **i32) for _ in range(2))
+        self._before[-1] = n_pages
+        self._behind[-1] = n_pages
+        plan = B.empty_kv_plan(n_req, 0, device=dev)
+        self.plan = replace(plan, lens=self._behind[:n_req], ring=self._behind[n_req:])   # the last step's
         self._positions = torch.empty(max_tokens, **i32)
         self._slots = torch.empty(max_tokens, dtype=torch.int64, device=dev)
         self.x = torch.zeros((max_tokens, c.hidden), **f32)      # residual stream
@@ -273,11 +274,6 @@ class BatchDecoder:
         self.argmax_ws = torch.empty(B.qdec_argmax_rows_workspace_bytes(n_req), dtype=torch.uint8, device=dev)
         self.scale = 1.0 / math.sqrt(c.head_dim)
 
-    @property
-    def plan(self) -> B.KvPlan:
-        """The last step's plan (lens, refused, offsets, ...)."""
-        return self.plans[self.turn ^ 1]
-
     def step(self, tokens: torch.Tensor, new_lens: torch.Tensor, stream=None) -> None:
         """tokens: int32 [T] on the device, T <= max_tokens, the requests' new
         tokens one after the other in the order of the slots (places behind
@@ -295,12 +291,13 @@ class BatchDecoder:
         x, h, y = self.x[:t], self.h[1:1 + t], None
         ws = self.ws_plain if self.prefix is None else self.ws
         B.qdec_embed_rows(self.emb, tokens, out=x, stream=s)
-        before, own = self.plans[self.turn ^ 1], self.plans[self.turn]
-        plan = B.KvPlan(own.lens, own.kv_lens, own.offsets, self._positions[:t], self._slots[:t], own.ring, own.refused)
-        B.qkv_plan(before.lens, new_lens, self.tables, self.free_ring, before.ring, self.page_size, t,
+        plan = replace(self.plan, positions=self._positions[:t], slots=self._slots[:t])
+        n = self.n_req
+        B.qkv_plan(self._before[:n], new_lens, self.tables, self.free_ring, self._before[n:], self.page_size, t,
                    prefix_pages=0 if self.prefix is None else self.prefix.numel(), out=plan, stream=s)
-        self.plans[self.turn] = plan                             # (a refused call leaves everything as it was)
-        self.turn ^= 1
+        self.plan = plan                                         # (a refused call leaves everything as it was)
+        with torch.cuda.stream(s):
+            self._before.copy_(self._behind)
         for li, ly in enumerate(self.layers):
             B.qdec_rmsnorm(x, ly.attn_norm, c.eps, residual=y, out=h, stream=s)
             q, k, v = B.qmatmul_gemm_grouped([ly.wq, ly.wk, ly.wv], h, outs=[self.q[:t], self.k[:t], self.v[:t]],
