@@ -264,7 +264,8 @@ class BatchDecoder:
         self.y_attn, self.y_ffn = (torch.zeros((max_tokens, c.hidden), **f32) for _ in range(2))
         self.g16 = torch.zeros((max_tokens, c.inter), **f16)
         self.last = torch.zeros((n_req, c.hidden), **f32)
-        self.last16 = torch.zeros((n_req, c.hidden), **f16)
+        # Normed last token: of the rows of this step, and of every request's last step with tokens.
+        self.step16, self.last16 = (torch.zeros((n_req, c.hidden), **f16) for _ in range(2))
         self.logits = torch.zeros((n_req, c.vocab), **f32)
         self.token = torch.zeros(n_req, **i32)                   # greedy next token of every request
         self.ws = torch.empty(B.qattn_paged_workspace_bytes(c.n_q_heads, c.n_kv_heads, c.head_dim, n_req, max_tokens, 1),
@@ -280,9 +281,10 @@ class BatchDecoder:
         the last one count nothing); new_lens: int32 [n_req], how many each
         request has (0: none; -1: it has ended, its pages are free from the
         next step on).  Leaves logits and the greedy next token of every
-        request with new tokens in self.logits[i] and self.token[i].  A request
-        that finds no pages is refused (self.plan.refused, kv_lens 0): its
-        tokens are not cached and its logits are of no use."""
+        request with new tokens in self.logits[i] and self.token[i]; the others
+        keep theirs.  A request that finds no pages is refused
+        (self.plan.refused, kv_lens 0): its tokens are not cached, and it keeps
+        its logits and next token too, so the same tokens can come again."""
         c, s, t = self.cfg, stream, tokens.numel()
         if not 1 <= t <= self.max_tokens:
             raise ValueError(f"a step of {t} tokens: must be 1 .. max_tokens={self.max_tokens}")
@@ -313,7 +315,10 @@ class BatchDecoder:
             y = B.qmatmul_gemm(ly.wd, self.g16[:t], out=self.y_ffn[:t], stream=s)
         B.qdec_rmsnorm(x, self.norm, c.eps, residual=y, out=h, stream=s)
         B.qdec_embed_rows(self.h[:1 + t], plan.offsets[1:], out=self.last, stream=s)
-        B.qdec_cast_f16(self.last, out=self.last16, stream=s)
+        B.qdec_cast_f16(self.last, out=self.step16, stream=s)
+        with torch.cuda.stream(s):
+            served = torch.minimum(new_lens, plan.kv_lens) > 0   # new tokens, and not refused
+            torch.where(served[:, None], self.step16, self.last16, out=self.last16)
         B.qmatmul_gemm(self.lm_head, self.last16, out=self.logits, stream=s)
         B.qdec_argmax_rows(self.logits, out=self.token, workspace=self.argmax_ws, stream=s)
 
