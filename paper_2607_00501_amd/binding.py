@@ -140,6 +140,20 @@ def _stream(stream=None):
     return _raw_stream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
+def _empty(shape, dtype, device, stream=None, scratch=False) -> torch.Tensor:
+    """Memory of a call that goes to `stream`, from that stream's blocks: one of
+    the current stream's may still be in use there when the call begins, or be
+    handed out there again before it ends.  The caller reads an output on the
+    current stream as well; scratch ends with the call."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if not scratch:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 @dataclass
 class QWeight:
     """A quantised tensor [batch][n][k]: codes and fp16 scale bits in torch
@@ -622,9 +636,9 @@ def qdec_argmax_rows(logits: torch.Tensor, out: Optional[torch.Tensor] = None,
     rows, n = logits.shape
     _tensors(logits=(logits, torch.float32, (rows, n)))
     if out is None:
-        out = torch.empty(rows, dtype=torch.int32, device=logits.device)
+        out = _empty(rows, torch.int32, logits.device, stream)
     if workspace is None:
-        workspace = torch.empty(qdec_argmax_rows_workspace_bytes(rows), dtype=torch.uint8, device=logits.device)
+        workspace = _empty(qdec_argmax_rows_workspace_bytes(rows), torch.uint8, logits.device, stream, scratch=True)
     _tensors(out=(out, torch.int32, (rows,)), workspace=(workspace, torch.uint8, None))
     _check(lib().qdec_argmax_rows(_ptr(logits), rows, n, _ptr(out), _ptr(workspace), workspace.numel(),
                                   _stream(stream)))
@@ -670,9 +684,9 @@ class KvPlan:
                  ring=(self.ring, i32, (2,)), refused=(self.refused, i32, (1,)))
 
 
-def empty_kv_plan(n_req: int, max_tokens: int, device="cuda") -> KvPlan:
+def empty_kv_plan(n_req: int, max_tokens: int, device="cuda", stream=None) -> KvPlan:
     def ints(n, dtype=torch.int32):
-        return torch.empty(n, dtype=dtype, device=device)
+        return _empty(n, dtype, device, stream)
     return KvPlan(ints(n_req), ints(n_req), ints(n_req + 1), ints(max_tokens), ints(max_tokens, torch.int64), ints(2),
                   ints(1))
 
@@ -686,7 +700,7 @@ def qkv_plan(lens: torch.Tensor, new_lens: torch.Tensor, tables: torch.Tensor, f
     n_req, max_pages = tables.shape
     n_pages = free_ring.numel()
     if out is None:
-        out = empty_kv_plan(n_req, max_tokens, tables.device)
+        out = empty_kv_plan(n_req, max_tokens, tables.device, stream)
     elif out.lens.numel() != n_req or out.positions.numel() != max_tokens or out.lens.device != tables.device:
         raise ValueError(f"out: a plan of {out.lens.numel()} requests and {out.positions.numel()} tokens on "
                          f"{out.lens.device}, need {n_req} and {max_tokens} on {tables.device}")
@@ -712,7 +726,7 @@ def qkv_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions
     hq = q.shape[1] // d
     f32, f16 = torch.float32, torch.float16
     if q_out is None:
-        q_out = torch.empty((t, hq, d), dtype=f16, device=q.device)
+        q_out = _empty((t, hq, d), f16, q.device, stream)
     _tensors(q=(q, f32, (t, hq * d)), k=(k, f32, (t, hkv * d)), v=(v, f32, (t, hkv * d)),
              positions=(positions, torch.int32, (t,)), slots=(slots, torch.int64, (t,)),
              table=(table, f32, (table.shape[0], d // 2, 2)), k_pages=(k_pages, f16, None),
@@ -747,10 +761,10 @@ def qattn_paged_f16(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     f16, i32 = torch.float16, torch.int32
     shared = 0 if prefix is None else prefix.numel()
     if out is None:
-        out = torch.empty((t, hq * d), dtype=f16, device=q.device)
+        out = _empty((t, hq * d), f16, q.device, stream)
     if workspace is None:
         nb = qattn_paged_workspace_bytes(hq, hkv, d, n_req, t, shared)
-        workspace = torch.empty(max(nb, 16), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(nb, 16), torch.uint8, q.device, stream, scratch=True)
     _tensors(q=(q, f16, (t, hq, d)), k_pages=(k_pages, f16, None), v_pages=(v_pages, f16, k_pages.shape),
              tables=(tables, i32, None), offsets=(offsets, i32, (n_req + 1,)), kv_lens=(kv_lens, i32, (n_req,)),
              prefix=(prefix, i32, (shared,)), out=(out, f16, (t, hq * d)),
