@@ -186,11 +186,11 @@ def qm_weight_bytes(fmt: int, layout: int, batch: int, n: int, k: int):
     return qb.value, sb.value
 
 
-def empty_qweight(fmt: int, layout: int, batch: int, n: int, k: int, device="cuda") -> QWeight:
+def empty_qweight(fmt: int, layout: int, batch: int, n: int, k: int, device="cuda", stream=None) -> QWeight:
     qb, sb = qm_weight_bytes(fmt, layout, batch, n, k)
     return QWeight(fmt, layout, batch, n, k,
-                   torch.empty(max(qb, 1), dtype=torch.uint8, device=device),
-                   torch.empty(max(sb // 2, 1), dtype=torch.int16, device=device))
+                   _empty(max(qb, 1), torch.uint8, device, stream),
+                   _empty(max(sb // 2, 1), torch.int16, device, stream))
 
 
 def qm_quantise(w: torch.Tensor, fmt: int, out: Optional[QWeight] = None, stream=None) -> QWeight:
@@ -201,21 +201,21 @@ def qm_quantise(w: torch.Tensor, fmt: int, out: Optional[QWeight] = None, stream
         batch, n, k = w.shape
     assert w.dtype == torch.float32 and w.is_contiguous()
     if out is None:
-        out = empty_qweight(fmt, LAYOUT_CANONICAL, batch, n, k, w.device)
+        out = empty_qweight(fmt, LAYOUT_CANONICAL, batch, n, k, w.device, stream)
     _check(lib().qm_quantise(fmt, _ptr(w), ctypes.byref(out.c()), _stream(stream)))
     return out
 
 
 def qm_dequantise(w: QWeight, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     if out is None:
-        out = torch.empty((w.batch, w.n, w.k), dtype=torch.float32, device=w.qdata.device)
+        out = _empty((w.batch, w.n, w.k), torch.float32, w.qdata.device, stream)
     _check(lib().qm_dequantise(ctypes.byref(w.c()), _ptr(out), _stream(stream)))
     return out
 
 
 def qm_repack(src: QWeight, layout: int, out: Optional[QWeight] = None, stream=None) -> QWeight:
     if out is None:
-        out = empty_qweight(src.format, layout, src.batch, src.n, src.k, src.qdata.device)
+        out = empty_qweight(src.format, layout, src.batch, src.n, src.k, src.qdata.device, stream)
     _check(lib().qm_repack(ctypes.byref(src.c()), ctypes.byref(out.c()), _stream(stream)))
     return out
 
@@ -224,7 +224,7 @@ def qmatmul_gemv(w: QWeight, x: torch.Tensor, out: Optional[torch.Tensor] = None
     """x: fp16 [k] -> fp32 [n]."""
     assert x.dtype == torch.float16 and x.is_contiguous() and x.numel() == w.k
     if out is None:
-        out = torch.empty(w.n, dtype=torch.float32, device=x.device)
+        out = _empty(w.n, torch.float32, x.device, stream)
     _check(lib().qmatmul_gemv(ctypes.byref(w.c()), _ptr(x), _ptr(out), _stream(stream)))
     return out
 
@@ -235,7 +235,7 @@ def qmatmul_gemv_swiglu(w_gate: QWeight, w_up: QWeight, x: torch.Tensor, out: Op
     an fp16 tensor)."""
     assert x.dtype == torch.float16 and x.is_contiguous() and x.numel() == w_gate.k
     if out is None:
-        out = torch.empty(w_gate.n, dtype=torch.float32, device=x.device)
+        out = _empty(w_gate.n, torch.float32, x.device, stream)
     fn = lib().qmatmul_gemv_swiglu_f16 if out.dtype == torch.float16 else lib().qmatmul_gemv_swiglu
     assert out.dtype in (torch.float16, torch.float32) and out.is_contiguous() and out.numel() == w_gate.n
     _check(fn(ctypes.byref(w_gate.c()), ctypes.byref(w_up.c()), _ptr(x), _ptr(out), _stream(stream)))
@@ -262,7 +262,7 @@ def qmatmul_gemv_grouped(ws, xs, outs=None, stream=None):
     for w, x in zip(ws, xs):
         assert x.dtype == torch.float16 and x.is_contiguous() and x.numel() == w.k
     if outs is None:
-        outs = [torch.empty(w.n, dtype=torch.float32, device=x.device) for w, x in zip(ws, xs)]
+        outs = [_empty(w.n, torch.float32, x.device, stream) for w, x in zip(ws, xs)]
     n, descs, xp, yp = gemv_group_args(ws, xs, outs)
     _check(lib().qmatmul_gemv_grouped(n, descs, xp, yp, _stream(stream)))
     return outs
@@ -277,7 +277,7 @@ def qmatmul_gemv_grouped_rmsnorm(ws, x: torch.Tensor, gain: torch.Tensor, eps: f
         assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == k
     assert gain.dtype == torch.float16 and gain.numel() == k
     if outs is None:
-        outs = [torch.empty(w.n, dtype=torch.float32, device=x.device) for w in ws]
+        outs = [_empty(w.n, torch.float32, x.device, stream) for w in ws]
     n = len(ws)
     descs = (CQWeight * n)(*[w.c() for w in ws])
     yp = (ctypes.c_void_p * n)(*[t.data_ptr() for t in outs])
@@ -296,7 +296,7 @@ def qmatmul_gemv_swiglu_rmsnorm_f16(w_gate: QWeight, w_up: QWeight, x: torch.Ten
         assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == k
     assert gain.dtype == torch.float16 and gain.numel() == k
     if out is None:
-        out = torch.empty(w_gate.n, dtype=torch.float16, device=x.device)
+        out = _empty(w_gate.n, torch.float16, x.device, stream)
     assert out.dtype == torch.float16 and out.numel() == w_gate.n
     _check(lib().qmatmul_gemv_swiglu_rmsnorm_f16(ctypes.byref(w_gate.c()), ctypes.byref(w_up.c()), _ptr(x),
                                                  _ptr(residual), _ptr(gain), eps, _ptr(x_out), _ptr(out),
@@ -310,7 +310,7 @@ def qdec_embed_rows(table: torch.Tensor, tokens: torch.Tensor, out: Optional[tor
     m = tokens.numel()
     assert tokens.dtype == torch.int32 and table.dtype == torch.float16
     if out is None:
-        out = torch.empty((m, hidden), dtype=torch.float32, device=table.device)
+        out = _empty((m, hidden), torch.float32, table.device, stream)
     _check(lib().qdec_embed_rows(_ptr(table), vocab, hidden, _ptr(tokens), m, _ptr(out), _stream(stream)))
     return out
 
@@ -342,7 +342,7 @@ def qdec_rope_append_rows(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, p0:
     assert k_cache.is_contiguous() and v_cache.is_contiguous()
     _check_head_gains(q_norm, k_norm, d)
     if q_out is None:
-        q_out = torch.empty((hq, m, d), dtype=torch.float16, device=q.device)
+        q_out = _empty((hq, m, d), torch.float16, q.device, stream)
     tlen = 0
     if table is not None:
         assert table.dtype == torch.float32 and table.is_contiguous() and table.shape[1:] == (d // 2, 2)
@@ -357,7 +357,7 @@ def qdec_heads_to_rows_f16(o: torch.Tensor, out: Optional[torch.Tensor] = None, 
     """fp32 [H][m][D] -> fp16 [m][H*D]."""
     h, m, d = o.shape
     if out is None:
-        out = torch.empty((m, h * d), dtype=torch.float16, device=o.device)
+        out = _empty((m, h * d), torch.float16, o.device, stream)
     _check(lib().qdec_heads_to_rows_f16(_ptr(o), h, m, d, _ptr(out), _stream(stream)))
     return out
 
@@ -366,14 +366,14 @@ def qdec_swiglu_f16(gate: torch.Tensor, up: torch.Tensor, out: Optional[torch.Te
     """fp16(silu(gate) * up), elementwise, fp32 in."""
     assert gate.dtype == up.dtype == torch.float32 and gate.shape == up.shape
     if out is None:
-        out = torch.empty(gate.shape, dtype=torch.float16, device=gate.device)
+        out = _empty(gate.shape, torch.float16, gate.device, stream)
     _check(lib().qdec_swiglu_f16(_ptr(gate), _ptr(up), gate.numel(), _ptr(out), _stream(stream)))
     return out
 
 
 def qdec_rope_table(max_len: int, head_dim: int, theta: float, device="cuda", stream=None) -> torch.Tensor:
     """fp32 [max_len][head_dim/2][2] (cos, sin) table."""
-    t = torch.empty((max_len, head_dim // 2, 2), dtype=torch.float32, device=device)
+    t = _empty((max_len, head_dim // 2, 2), torch.float32, device, stream)
     _check(lib().qdec_rope_table(max_len, head_dim, theta, _ptr(t), _stream(stream)))
     return t
 
@@ -383,7 +383,7 @@ def qdec_rope_table_llama3(max_len: int, head_dim: int, theta: float, scaling, d
     """The (cos, sin) table with the Llama 3 long-context frequencies;
     scaling = (factor, low_freq_factor, high_freq_factor, original_len)."""
     factor, low, high, orig = (float(v) for v in scaling)
-    t = torch.empty((max_len, head_dim // 2, 2), dtype=torch.float32, device=device)
+    t = _empty((max_len, head_dim // 2, 2), torch.float32, device, stream)
     _check(lib().qdec_rope_table_llama3(max_len, head_dim, theta, factor, low, high, orig, _ptr(t), _stream(stream)))
     return t
 
@@ -420,7 +420,7 @@ def qmatmul_gemm(w: QWeight, x: torch.Tensor, out: Optional[torch.Tensor] = None
     assert x.dtype == torch.float16 and x.is_contiguous() and x.dim() == 2 and x.shape[1] == w.k
     m = x.shape[0]
     if out is None:
-        out = torch.empty((m, w.n), dtype=torch.float32, device=x.device)
+        out = _empty((m, w.n), torch.float32, x.device, stream)
     _check(lib().qmatmul_gemm(ctypes.byref(w.c()), _ptr(x), m, _ptr(out), _stream(stream)))
     return out
 
@@ -441,7 +441,7 @@ def qmatmul_gemm_grouped(ws, x: torch.Tensor, outs=None, stream=None):
     for w in ws:
         assert x.shape[1] == w.k
     if outs is None:
-        outs = [torch.empty((m, w.n), dtype=torch.float32, device=x.device) for w in ws]
+        outs = [_empty((m, w.n), torch.float32, x.device, stream) for w in ws]
     n, descs, yp = gemm_group_args(ws, outs)
     _check(lib().qmatmul_gemm_grouped(n, descs, _ptr(x), m, yp, _stream(stream)))
     return outs
@@ -453,7 +453,7 @@ def qmatmul_gemm_swiglu_f16(w_gate: QWeight, w_up: QWeight, x: torch.Tensor, out
     assert x.dtype == torch.float16 and x.is_contiguous() and x.dim() == 2 and x.shape[1] == w_gate.k
     m = x.shape[0]
     if out is None:
-        out = torch.empty((m, w_gate.n), dtype=torch.float16, device=x.device)
+        out = _empty((m, w_gate.n), torch.float16, x.device, stream)
     assert out.dtype == torch.float16 and out.is_contiguous() and out.numel() == m * w_gate.n
     _check(lib().qmatmul_gemm_swiglu_f16(ctypes.byref(w_gate.c()), ctypes.byref(w_up.c()), _ptr(x), m, _ptr(out),
                                          _stream(stream)))
@@ -476,10 +476,10 @@ def qattn_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, 
     assert q.dtype == k_cache.dtype == v_cache.dtype == torch.float16
     assert q.is_contiguous() and k_cache.is_contiguous() and v_cache.is_contiguous()
     if out is None:
-        out = torch.empty((hq, d), dtype=torch.float32, device=q.device)
+        out = _empty((hq, d), torch.float32, q.device, stream)
     nb = qattn_decode_workspace_bytes(hq, d)
     if workspace is None:
-        workspace = torch.empty(nb, dtype=torch.uint8, device=q.device)
+        workspace = _empty(nb, torch.uint8, q.device, stream, scratch=True)
     assert out.dtype in (torch.float16, torch.float32) and out.is_contiguous() and out.numel() == hq * d
     fn = lib().qattn_decode_f16 if out.dtype == torch.float16 else lib().qattn_decode
     _check(fn(_ptr(q), _ptr(k_cache), _ptr(v_cache), hq, hkv, d, length, max_len, scale,
@@ -509,11 +509,11 @@ def qattn_prefill(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
     assert q.dtype == k_cache.dtype == v_cache.dtype == torch.float16
     assert q.is_contiguous() and k_cache.is_contiguous() and v_cache.is_contiguous()
     if out is None:
-        out = torch.empty((hq, m, d), dtype=torch.float32, device=q.device)
+        out = _empty((hq, m, d), torch.float32, q.device, stream)
     assert out.dtype == torch.float32 and out.is_contiguous() and out.numel() == hq * m * d
     if workspace is None:
         nb = qattn_prefill_workspace_bytes(hq, d, m, p0)
-        workspace = torch.empty(max(nb, 16), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(nb, 16), torch.uint8, q.device, stream, scratch=True)
     if workspace is NO_WORKSPACE:
         wp, wn = None, 0
     else:
@@ -534,11 +534,11 @@ def qattn_prefill_rows_f16(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torc
     assert q.dtype == k_cache.dtype == v_cache.dtype == torch.float16
     assert q.is_contiguous() and k_cache.is_contiguous() and v_cache.is_contiguous()
     if out is None:
-        out = torch.empty((m, hq * d), dtype=torch.float16, device=q.device)
+        out = _empty((m, hq * d), torch.float16, q.device, stream)
     assert out.dtype == torch.float16 and out.is_contiguous() and out.numel() == hq * m * d
     if workspace is None:
         nb = qattn_prefill_workspace_bytes(hq, d, m, p0)
-        workspace = torch.empty(max(nb, 16), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(nb, 16), torch.uint8, q.device, stream, scratch=True)
     if workspace is NO_WORKSPACE:
         wp, wn = None, 0
     else:
@@ -554,7 +554,7 @@ def qdec_embed(table: torch.Tensor, token: torch.Tensor, out: Optional[torch.Ten
     vocab, hidden = table.shape
     assert table.dtype == torch.float16 and table.is_contiguous() and token.dtype == torch.int32
     if out is None:
-        out = torch.empty(hidden, dtype=torch.float32, device=table.device)
+        out = _empty(hidden, torch.float32, table.device, stream)
     _check(lib().qdec_embed(_ptr(table), vocab, hidden, _ptr(token), _ptr(out), _stream(stream)))
     return out
 
@@ -569,7 +569,7 @@ def qdec_rmsnorm(x: torch.Tensor, w: torch.Tensor, eps: float, residual: Optiona
     if residual is not None:
         assert residual.dtype == torch.float32 and residual.shape == x.shape and residual.is_contiguous()
     if out is None:
-        out = torch.empty(x.shape, dtype=torch.float16, device=x.device)
+        out = _empty(x.shape, torch.float16, x.device, stream)
     _check(lib().qdec_rmsnorm(_ptr(x), _ptr(residual), _ptr(w), rows, hidden, eps, _ptr(out), _stream(stream)))
     return out
 
@@ -588,7 +588,7 @@ def qdec_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: int
     assert k_cache.is_contiguous() and v_cache.is_contiguous()
     _check_head_gains(q_norm, k_norm, d)
     if q_out is None:
-        q_out = torch.empty((hq, d), dtype=torch.float16, device=q.device)
+        q_out = _empty((hq, d), torch.float16, q.device, stream)
     tlen = 0
     if table is not None:
         assert table.dtype == torch.float32 and table.is_contiguous() and table.shape[1:] == (d // 2, 2)
@@ -603,7 +603,7 @@ def qdec_cast_f16(x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=No
     """fp32 -> fp16 (round to nearest even), any shape."""
     assert x.dtype == torch.float32 and x.is_contiguous()
     if out is None:
-        out = torch.empty(x.shape, dtype=torch.float16, device=x.device)
+        out = _empty(x.shape, torch.float16, x.device, stream)
     _check(lib().qdec_cast_f16(_ptr(x), x.numel(), _ptr(out), _stream(stream)))
     return out
 
@@ -616,9 +616,9 @@ def qdec_argmax(logits: torch.Tensor, out: Optional[torch.Tensor] = None, worksp
     """fp32 [n] -> int32 [1] on the device (lowest index among equal maxima)."""
     assert logits.dtype == torch.float32 and logits.is_contiguous()
     if out is None:
-        out = torch.empty(1, dtype=torch.int32, device=logits.device)
+        out = _empty(1, torch.int32, logits.device, stream)
     if workspace is None:
-        workspace = torch.empty(ARGMAX_WORKSPACE_BYTES, dtype=torch.uint8, device=logits.device)
+        workspace = _empty(ARGMAX_WORKSPACE_BYTES, torch.uint8, logits.device, stream, scratch=True)
     _check(lib().qdec_argmax(_ptr(logits), logits.numel(), _ptr(out), _ptr(workspace), workspace.numel(),
                              _stream(stream)))
     return out
@@ -796,11 +796,9 @@ def qmoe_route(logits: torch.Tensor, top_k: int, out: Optional[Routing] = None, 
     assert logits.dtype == torch.float32 and logits.is_contiguous()
     dev = logits.device
     if out is None:
-        out = Routing(torch.empty((m, top_k), dtype=torch.int32, device=dev),
-                      torch.empty((m, top_k), dtype=torch.float32, device=dev),
-                      torch.empty(e, dtype=torch.int32, device=dev),
-                      torch.empty(e + 1, dtype=torch.int32, device=dev),
-                      torch.empty(max(m * top_k, 1), dtype=torch.int32, device=dev), top_k)
+        out = Routing(_empty((m, top_k), torch.int32, dev, stream), _empty((m, top_k), torch.float32, dev, stream),
+                      _empty(e, torch.int32, dev, stream), _empty(e + 1, torch.int32, dev, stream),
+                      _empty(max(m * top_k, 1), torch.int32, dev, stream), top_k)
     _check(lib().qmoe_route(_ptr(logits), m, e, top_k, _ptr(out.ids), _ptr(out.gates), _ptr(out.counts),
                             _ptr(out.offsets), _ptr(out.sorted_assign), _stream(stream)))
     return out
@@ -812,10 +810,10 @@ def qmoe_grouped_gemm(w_gate: QWeight, w_up: QWeight, w_down: QWeight, x: torch.
     m, hidden = x.shape
     assert x.dtype == torch.float16 and x.is_contiguous()
     if out is None:
-        out = torch.empty((m, hidden), dtype=torch.float32, device=x.device)
+        out = _empty((m, hidden), torch.float32, x.device, stream)
     if workspace is None:
         nb = qmoe_workspace_bytes(m, w_gate.batch, r.top_k, hidden, w_gate.n)
-        workspace = torch.empty(max(nb, 16), dtype=torch.uint8, device=x.device)
+        workspace = _empty(max(nb, 16), torch.uint8, x.device, stream, scratch=True)
     _check(lib().qmoe_grouped_gemm(ctypes.byref(w_gate.c()), ctypes.byref(w_up.c()), ctypes.byref(w_down.c()),
                                    _ptr(x), m, r.top_k, _ptr(r.ids), _ptr(r.gates), _ptr(r.counts), _ptr(r.offsets),
                                    _ptr(r.sorted_assign), _ptr(out), _ptr(workspace), workspace.numel(),
@@ -834,7 +832,7 @@ def qmoe_grouped_gemm_noalloc(w_gate: QWeight, w_up: QWeight, w_down: QWeight, x
     m, hidden = x.shape
     assert x.dtype == torch.float16 and x.is_contiguous()
     if out is None:
-        out = torch.empty((m, hidden), dtype=torch.float32, device=x.device)
+        out = _empty((m, hidden), torch.float32, x.device, stream)
     _check(lib().qmoe_grouped_gemm_noalloc(ctypes.byref(w_gate.c()), ctypes.byref(w_up.c()),
                                            ctypes.byref(w_down.c()), _ptr(x), m, r.top_k, _ptr(r.ids),
                                            _ptr(r.gates), _ptr(r.counts), _ptr(r.offsets), _ptr(r.sorted_assign),
