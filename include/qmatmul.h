@@ -529,7 +529,8 @@ qm_status qdec_argmax_rows(const float* logits, int64_t rows, int64_t n, int32_t
  *    ring's last entry, in request order, free from the next step on.
  *  - ring_out = the ring's head and count after the step.
  * tables and free_ring are changed in place, and the same call repeated (same
- * lens, ring) does the same.  lens_out and ring_out must not be lens and ring.
+ * lens, ring) does the same.  What is written must not overlap another buffer of
+ * the call (lens_out and ring_out are not lens and ring).
  * A length below 0 or past the table is refused, its pages are not given back;
  * a ring that is none of this size counts as empty.
  * 0 <= max_tokens <= 65536; 0 <= prefix_pages <= max_pages.  int32 pointers

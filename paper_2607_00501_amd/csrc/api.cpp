@@ -59,6 +59,26 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 bool aligned2(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 1u) == 0; }
 
+// A buffer of a call, and whether the call writes it.
+struct Span {
+  const char* name;
+  const void* p;
+  uint64_t bytes;
+  bool written;
+};
+
+// Refuses a call one of whose written buffers shares bytes with another buffer.
+template <size_t N>
+qm_status check_disjoint(const char* call, const Span (&s)[N]) {
+  for (size_t i = 0; i < N; ++i)
+    for (size_t j = 0; j < i; ++j) {
+      const uint64_t a = reinterpret_cast<uintptr_t>(s[i].p), b = reinterpret_cast<uintptr_t>(s[j].p);
+      if ((s[i].written || s[j].written) && s[i].p && s[j].p && a < b + s[j].bytes && b < a + s[i].bytes)
+        return fail(QM_EINVAL, "%s: %s and %s must not overlap", call, s[j].name, s[i].name);
+    }
+  return QM_OK;
+}
+
 qm_status check_weight(const qm_qweight* w, const char* name) {
   if (!w) return fail(QM_EINVAL, "%s: null weight descriptor", name);
   if (!fmt_valid(w->format)) return fail(QM_EFORMAT, "%s: unknown format %d", name, w->format);
@@ -833,6 +853,15 @@ qm_status qkv_plan(const int32_t* lens, const int32_t* new_lens, int64_t n_req, 
   for (const void* p : ints)
     if (!aligned4(p)) return fail(QM_EALIGN, "%s: pointers must be 4-byte aligned", name);
   if (!aligned8(slots)) return fail(QM_EALIGN, "%s: slots must be 8-byte aligned", name);
+  // (Every workgroup reads all lengths and the ring; the first one writes the next ones.)
+  const uint64_t n = static_cast<uint64_t>(n_req), t = static_cast<uint64_t>(max_tokens);
+  const Span spans[] = {{"lens", lens, 4 * n, false}, {"new_lens", new_lens, 4 * n, false}, {"ring", ring, 8, false},
+                        {"tables", tables, 4 * n * static_cast<uint64_t>(max_pages), true},
+                        {"free_ring", free_ring, 4 * static_cast<uint64_t>(n_pages), true},
+                        {"lens_out", lens_out, 4 * n, true}, {"kv_lens", kv_lens, 4 * n, true},
+                        {"offsets", offsets, 4 * n + 4, true}, {"positions", positions, 4 * t, true},
+                        {"slots", slots, 8 * t, true}, {"ring_out", ring_out, 8, true}, {"refused", refused, 4, true}};
+  if ((st = check_disjoint(name, spans)) != QM_OK) return st;
   a.lens = lens; a.new_lens = new_lens; a.tables = tables; a.free_ring = free_ring; a.ring = ring;
   a.lens_out = lens_out; a.kv_lens = kv_lens; a.offsets = offsets; a.positions = positions; a.slots = slots;
   a.ring_out = ring_out; a.refused = refused;
