@@ -550,6 +550,7 @@ qm_status qkv_plan(const int32_t* lens, const int32_t* new_lens, int64_t n_req, 
  * table: (cos, sin) pairs of table_len positions (qdec_rope_table).  A token
  * whose slot is not in the pools or whose position is not in the table (-1)
  * writes nothing; no two tokens may have the same slot.  head_dim 64 or 128.
+ * q_out and the pools must not overlap each other or another buffer of the call.
  * q, k, v 16-byte, positions 4-byte, the others 8-byte aligned.
  * (Sec. 3.2: RoPE and the KV cache.) */
 qm_status qkv_rope_append(const float* q, const float* k, const float* v, int32_t n_q_heads, int32_t n_kv_heads,
@@ -574,9 +575,10 @@ qm_status qkv_rope_append(const float* q, const float* k, const float* v, int32_
  * page_size; others are held within these limits, and the rows of what then is
  * no request may hold anything.
  * q: fp16 [tokens][n_q_heads][head_dim]; out: fp16 [tokens][n_q_heads *
- * head_dim] (the output projection's rows), not q; rows past offsets[n_req] are
- * left as they were.  head_dim 64 or 128; n_kv_heads <= 128; n_q_heads <= 1024,
- * a multiple of it, at most 128 times; 0 <= tokens <= 65536; scale finite and
+ * head_dim] (the output projection's rows); it and the workspace must not
+ * overlap another buffer of the call; rows past offsets[n_req] are left as they
+ * were.  head_dim 64 or 128; n_kv_heads <= 128; n_q_heads <= 1024, a multiple of
+ * it, at most 128 times; 0 <= tokens <= 65536; scale finite and
  * > 0.  A page id outside [0, n_pages) among the keys of a request (or of the
  * prefix) makes rows that see them, up to 128 (token, head) pairs at a time,
  * NaN (no host synchronisation, so no status code).  Scores, maxima and sums in

@@ -73,7 +73,7 @@ qm_status check_disjoint(const char* call, const Span (&s)[N]) {
   for (size_t i = 0; i < N; ++i)
     for (size_t j = 0; j < i; ++j) {
       const uint64_t a = reinterpret_cast<uintptr_t>(s[i].p), b = reinterpret_cast<uintptr_t>(s[j].p);
-      if ((s[i].written || s[j].written) && s[i].p && s[j].p && a < b + s[j].bytes && b < a + s[i].bytes)
+      if ((s[i].written || s[j].written) && a && b && s[i].bytes && s[j].bytes && a < b + s[j].bytes && b < a + s[i].bytes)
         return fail(QM_EINVAL, "%s: %s and %s must not overlap", call, s[j].name, s[i].name);
     }
   return QM_OK;
@@ -896,6 +896,15 @@ qm_status qkv_rope_append(const float* q, const float* k, const float* v, int32_
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned8(q_out) || !aligned8(k_pages) || !aligned8(v_pages) ||
       !aligned8(table) || !aligned8(slots) || !aligned4(positions))
     return fail(QM_EALIGN, "%s: q, k, v 16-byte, q_out, pools, table and slots 8-byte, positions 4-byte aligned", name);
+  const uint64_t t = static_cast<uint64_t>(tokens), qn = t * n_q_heads * head_dim, kn = t * n_kv_heads * head_dim;
+  const uint64_t pool = 2 * static_cast<uint64_t>(n_pages) * n_kv_heads * page_size * head_dim;
+  const Span spans[] = {{"q", q, 4 * qn, false}, {"k", k, 4 * kn, false}, {"v", v, 4 * kn, false},
+                        {"positions", positions, 4 * t, false}, {"slots", slots, 8 * t, false},
+                        {"table", table, 4 * static_cast<uint64_t>(table_len) * head_dim, false},
+                        {"q_norm", q_norm, 2 * static_cast<uint64_t>(head_dim), false},
+                        {"k_norm", k_norm, 2 * static_cast<uint64_t>(head_dim), false},
+                        {"q_out", q_out, 2 * qn, true}, {"k_pages", k_pages, pool, true}, {"v_pages", v_pages, pool, true}};
+  if ((st = check_disjoint(name, spans)) != QM_OK) return st;
   a.q = q; a.k = k; a.v = v; a.positions = positions; a.slots = slots;
   a.table = reinterpret_cast<const float2*>(table); a.table_len = table_len;
   a.q_gain = q_norm; a.k_gain = k_norm; a.eps = eps;
@@ -947,13 +956,23 @@ qm_status qattn_paged_f16(const uint16_t* q, const uint16_t* k_pages, const uint
     return fail(QM_EALIGN, "%s: q, pools, out and workspace must be 16-byte aligned", name);
   if (!aligned4(tables) || !aligned4(prefix) || !aligned4(offsets) || !aligned4(kv_lens))
     return fail(QM_EALIGN, "%s: tables, prefix, offsets and kv_lens must be 4-byte aligned", name);
-  if (out == q) return fail(QM_EINVAL, "%s: out must not be q (several workgroups read a row)", name);
+  // (Several workgroups read a row of q while others have written theirs.)
+  const uint64_t row = 2 * static_cast<uint64_t>(n_q_heads) * head_dim, n = static_cast<uint64_t>(n_req);
+  const uint64_t pool = 2 * static_cast<uint64_t>(n_pages) * n_kv_heads * page_size * head_dim;
+  Span spans[] = {{"q", q, tokens * row, false}, {"k_pages", k_pages, pool, false}, {"v_pages", v_pages, pool, false},
+                  {"tables", tables, 4 * n * static_cast<uint64_t>(max_pages), false},
+                  {"prefix", prefix, 4 * static_cast<uint64_t>(prefix_pages), false},
+                  {"offsets", offsets, 4 * n + 4, false}, {"kv_lens", kv_lens, 4 * n, false},
+                  {"out", out, tokens * row, true}, {"workspace", workspace, 0, true}};
+  if ((st = check_disjoint(name, spans)) != QM_OK) return st;
   const DeviceInfo* d;
   if ((st = device_info(&d)) != QM_OK) return st;
   const size_t need =
       attn_paged_workspace_bytes(n_q_heads, n_kv_heads, head_dim, tokens, prefix_pages > 0, d->cu_count);
   if (!workspace || ws_bytes < need)
     return fail(QM_EWORKSPACE, "%s: workspace of %zu bytes needed (got %zu)", name, need, workspace ? ws_bytes : 0);
+  spans[8].bytes = need;
+  if ((st = check_disjoint(name, spans)) != QM_OK) return st;
   a.q = q; a.k_pages = k_pages; a.v_pages = v_pages; a.tables = tables; a.prefix = prefix;
   a.offsets = offsets; a.kv_lens = kv_lens; a.out = out; a.ws = static_cast<float*>(workspace);
   a.scale_log2 = scale * 1.4426950408889634f;
