@@ -246,6 +246,7 @@ class BatchDecoder:
         self.tables = torch.full((n_req, max_pages), -1, **i32)
         self.free_ring = torch.arange(n_pages, **i32)            # every page is free
         self.prefix: Optional[torch.Tensor] = None               # page ids that all requests share
+        self._captured = False                                   # a graph holds a step (with this prefix)
         # Lengths, and the free ring's head and count, before a step and behind it: qkv_plan writes other
         # places than it reads, and the step brings its result back to where the next one looks.
         self._before, self._behind = (torch.zeros(n_req + 2, **i32) for _ in range(2))
@@ -300,6 +301,7 @@ class BatchDecoder:
         self.plan = plan                                         # (a refused call leaves everything as it was)
         with torch.cuda.stream(s):
             self._before.copy_(self._behind)
+            self._captured = self._captured or torch.cuda.is_current_stream_capturing()
         for li, ly in enumerate(self.layers):
             B.qdec_rmsnorm(x, ly.attn_norm, c.eps, residual=y, out=h, stream=s)
             q, k, v = B.qmatmul_gemm_grouped([ly.wq, ly.wk, ly.wv], h, outs=[self.q[:t], self.k[:t], self.v[:t]],
@@ -323,12 +325,14 @@ class BatchDecoder:
         B.qdec_argmax_rows(self.logits, out=self.token, workspace=self.argmax_ws, stream=s)
 
     def share_prefix(self, tokens: torch.Tensor, stream=None) -> None:
-        """Before any other step: runs tokens (int32 [n] on the device, n a
-        multiple of page_size) once and keeps them as the beginning of every
-        request.  Waits for the device."""
+        """Before any other step (or capture of one): runs tokens (int32 [n] on
+        the device, n a multiple of page_size) once and keeps them as the
+        beginning of every request.  Waits for the device."""
         n, pages = tokens.numel(), tokens.numel() // self.page_size
         if self.prefix is not None or n == 0 or n % self.page_size or n > self.tables.shape[1] * self.page_size:
             raise ValueError(f"a prefix of {n} tokens: one, of whole pages of {self.page_size}, within max_len")
+        if self._captured:
+            raise ValueError("a prefix comes before a step is captured: the graph goes on without it")
         with torch.cuda.stream(stream):
             if self.plan.lens.any().item() or self.plan.ring[1].item() < pages:
                 raise ValueError(f"a prefix comes before any other step and has to find its {pages} pages")

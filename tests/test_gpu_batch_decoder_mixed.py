@@ -65,3 +65,19 @@ def test_replays_and_eager_steps_in_any_order(steps, prefix):
         assert torch.equal(decs[0].logits, decs[1].logits) and torch.equal(decs[0].token, decs[1].token)
         pages = [p for i in range(n) for p in decs[0].tables[i, prefix // 16:-(-lens[i] // 16)].tolist()]
         assert len(set(pages)) == len(pages)                         # no page has two owners
+
+
+def test_no_prefix_behind_a_captured_step():
+    """The graph has none: its requests would begin without the prefix, and give its
+    pages back when they end."""
+    layers, emb, norm, head, _ = _model(TINY, 68)
+    dec = BatchDecoder(TINY, emb, layers, norm, head, n_req=2, n_pages=20, max_len=128, page_size=16, max_tokens=32)
+    ones, fed = torch.ones(2, **I32), torch.zeros(2, **I32)
+    dec.step(fed, ones)
+    dec.step(fed, -ones)                                             # (nothing is held)
+    g = _captured(dec, fed, ones)
+    with pytest.raises(ValueError, match="captured"):
+        dec.share_prefix(torch.zeros(16, **I32))
+    for _ in range(3):
+        g.replay()
+    assert dec.plan.lens.tolist() == [3, 3] and dec.prefix is None
