@@ -517,9 +517,12 @@ qm_status qdec_argmax_rows(const float* logits, int64_t rows, int64_t n, int32_t
  *    in request order, and they are written into tables from entry
  *    ceil(lens[i] / page_size) on.  It is refused when they are not there (as is
  *    every later request that needs any), when its tokens would pass
- *    max_pages x page_size or when they do not all fit in max_tokens.
- *  - lens_out[i] = lens[i] + new_lens[i] (refused: lens[i]; ended: 0);
- *    kv_lens[i] = lens[i] + new_lens[i] (refused or ended: 0), the keys that the
+ *    max_pages x page_size or when new_lens[0] + .. + new_lens[i], of those >= 0,
+ *    passes max_tokens: from there on every request that has not ended counts as
+ *    refused, one without new tokens too (it has nothing to lose by it).
+ *  - lens_out[i] = lens[i] + new_lens[i] (refused: lens[i]; ended: 0), where a
+ *    lens[i] below the prefix counts as the prefix;
+ *    kv_lens[i] = the same sum (refused or ended: 0), the keys that the
  *    request's last token attends to; refused[0] = number of refused requests.
  *  - offsets (int32 [n_req + 1]): sums of the new_lens >= 0, at most max_tokens;
  *    refused requests keep their place.
@@ -531,7 +534,8 @@ qm_status qdec_argmax_rows(const float* logits, int64_t rows, int64_t n, int32_t
  * tables and free_ring are changed in place, and the same call repeated (same
  * lens, ring) does the same.  What is written must not overlap another buffer of
  * the call (lens_out and ring_out are not lens and ring).
- * A length below 0 or past the table is refused, its pages are not given back;
+ * A length below 0 or past the table is refused and left as it is, ended or not,
+ * and its pages are not given back;
  * a ring that is none of this size counts as empty.
  * 0 <= max_tokens <= 65536; 0 <= prefix_pages <= max_pages.  int32 pointers
  * 4-byte, slots 8-byte aligned.  Deterministic. */
@@ -567,7 +571,9 @@ qm_status qkv_rope_append(const float* q, const float* k, const float* v, int32_
  *   out[offsets[i] + j][h] = fp16_RNE(sum_{p<n} w_p v[g][p]),
  *   w = softmax_p(scale * q[h] . k[g][p]),  g = h / (n_q_heads / n_kv_heads);
  * a row that sees no key (kv_lens[i] = 0) is 0.  What lies past a row's keys
- * does not reach it, infinities and NaNs included.
+ * does not reach it, infinities and NaNs included; an infinite value that it
+ * sees makes that dimension infinite, or NaN where its weight is less than about
+ * 2^-32 of the row's largest.
  * prefix_pages > 0: positions below prefix_pages * page_size are read from the
  * pages prefix[0 .. prefix_pages), once for all requests, and the tables'
  * entries for them are not read; the other keys as before.
