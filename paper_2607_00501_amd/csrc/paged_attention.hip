@@ -52,7 +52,7 @@ __host__ __device__ __forceinline__ int tile_rows(int rows) { return rows <= kNa
 // rarely rescaled.  Weights go to the second product in fp16, rounded to nearest, as 2^7 w
 // relative to it: the largest is 2^15, and they keep 11 bits down to 2^-21.  Sums of
 // values and of (rounded) weights carry the same factor, in fp32.  Against 64 bits the
-// norm of the error is 2.5 .. 2.9e-4 of the output's with it, 2.07e-4 from the output's own
+// norm of the error is 2.4 .. 2.9e-4 of the output's with it, 2.07e-4 from the output's own
 // rounding to fp16.  A second fp16 term for what the rounding leaves takes that back for
 // twice the products: single tokens alone took 3 % (48 of 200 to 20,000 keys, 161 -> 166 us) to
 // 9 % (16 of 1,000, 22.1 -> 24.1) longer, and tiles are bound by their products already.
@@ -357,7 +357,7 @@ union TileLds {
 // limit: keys visible to this lane's row (lane & 15), 0 for rows that do not
 // exist.  acc[b][r]: dimension 16 b + 4 (lane / 16) + r of the row; m, l: its maximum
 // and sum of weights.  Bound by HBM: 48 single tokens after 200 to 20,000 keys, 870 MB
-// of keys in 149 us (16 / 8 heads of 128); one after 32,000, 131 MB in 33 with the join.
+// of keys in 155 us (16 / 8 heads of 128); one after 32,000, 131 MB in 33 with the join.
 template <int D>
 __device__ __forceinline__ void narrow_part(const PagedAttnArgs& a, _Float16* vl, const uint16_t* q_row, int limit,
                                             int head, const Keys& k, float4v (&acc)[D / 16], float& m, float& l) {
