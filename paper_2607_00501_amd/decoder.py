@@ -221,10 +221,12 @@ class BatchDecoder:
     Weights as for DenseDecoder.  n_req: requests at most (slots); n_pages:
     pages of page_size tokens that they share; max_len: tokens of one request
     at most (rounded up to pages); max_tokens: new tokens of one step at most,
-    all requests together.  Which request holds which pages, lengths and
+    all requests together (32,768 or fewer are run).  Which request holds which pages, lengths and
     positions live on the device (qkv_plan), and a step leaves them where it
     found them, so a step (or several) can be captured in a HIP graph and
-    replayed between eager steps in any order."""
+    replayed between eager steps in any order.  plan: the last step's lengths,
+    refusals, offsets and free ring, replayed or not; its positions and slots
+    are as many as the last call of step had tokens."""
 
     def __init__(self, cfg: DecoderConfig, emb: torch.Tensor, layers: List[LayerWeights], norm: torch.Tensor,
                  lm_head: B.QWeight, n_req: int, n_pages: int, max_len: int, page_size: int = 64,
